@@ -53,11 +53,19 @@ enum {
     LITHOS_OP_SPIN      = 10, /* test kernel: every block spins a fixed number of clock ticks */
     LITHOS_OP_ATTN_MERGE = 11, /* second step of a split ATTN_DEC: merges the key ranges' partial softmaxes */
     LITHOS_OP_SUM_SLICES = 12, /* second step of a K-sliced GEMM: adds the fp32 partial planes in slice order */
-    LITHOS_OP_ATTN_PREFILL = 13 /* causal self-attention over a whole prompt (query i sees keys 0..i), grouped-query */
+    LITHOS_OP_ATTN_PREFILL = 13, /* causal self-attention over a whole prompt (query i sees keys 0..i), grouped-query */
+    LITHOS_OP_GEMM_Q4   = 14, /* C = A dequant(W)^T [+bias][GELU][+residual] for few rows: weights in 4 bits, group scales */
+    LITHOS_OP_KV8_APPEND = 15, /* quantise new keys and values into a cache of 8 bits, a scale per block and head */
+    LITHOS_OP_ATTN_DEC8 = 16, /* ATTN_DEC against such a cache, with a length per sequence */
+    LITHOS_OP_LOGPROBS  = 17, /* per row of logits: log probability of a given token, entropy, log-sum-exp, top tokens */
+    LITHOS_OP_LOGPROBS_MERGE = 18, /* second step of a split LOGPROBS */
+    LITHOS_OP_LOGPROBS_GRAD = 19   /* gradient of log probability and entropy with respect to the logits */
 };
 
 #define LITHOS_ATTN_MAX_SPLITS 64
 #define LITHOS_GEMM_MAX_SLICES 64
+#define LITHOS_LOGPROBS_MAX_SPLITS 64
+#define LITHOS_LOGPROBS_MAX_TOP 32
 
 /* flags (meaning depends on the kind, see the table below) */
 #define LITHOS_F_TRANS_A   (1u << 0)   /* A is stored [K,M] */
@@ -72,6 +80,7 @@ enum {
 #define LITHOS_F_NORM_LN   (1u << 9)   /* GEMM: rows of A pass through LAYERNORM (gamma in[4], column sums in[5], eps fparam0) on load */
 #define LITHOS_F_NORM_RMS  (1u << 10)  /* GEMM: rows of A pass through RMSNORM (w in[4], eps fparam0) on load */
 #define LITHOS_F_GLU       (1u << 11)  /* GEMM: B holds N gate rows then N up rows; C = silu(A gate^T) * (A up^T) */
+#define LITHOS_F_E4M3      (1u << 12)  /* KV8_APPEND, ATTN_DEC8: the cache holds e4m3 codes (default int8) */
 
 /* GEMM tile selectors for lithos_op_t.tile (0 = library chooses, for SPLIT_A also 64x192 and 32x64 tiles) */
 #define LITHOS_TILE_64     64    /* 64x64 output tile */
@@ -122,6 +131,37 @@ enum {
  *             One workgroup per (pair of 128-query tiles, sequence, query head): tile p from the end and
  *             tile p from the start of the prompt, so that every block sees T/128 + 1 tiles of keys; grid
  *             x = heads of a key/value head x pairs, y = key/value head, z = sequence.
+ * GEMM_Q4     M,N,K,group                        A,codes,bias(f32),residual(f32),scales,[zeros] / C   ld0=lda, ld2=ldc, ld3=ldr
+ *             C[m,n] = sum_k A[m,k] s[n,k/group] (q[n,k] - z[n,k/group]); BIAS, GELU, RESIDUAL, GLU, IN_F32, OUT_F32 as for
+ *             GEMM (GLU: rows 0..N-1 of the weights are gates, N..2N-1 ups, N % 16 == 0).  group = 32, 64 or 128; K % 8 == 0.
+ *             codes: bytes [ceil(rows/16)][ceil(K/128)][4][16][16]: of 16 weight rows (fourth index) and 128 k, byte 4t + j of
+ *             piece p (third index) holds k = 32t + 8p + j in its low and k = 32t + 8p + j + 4 in its high half (t, j = 0..3);
+ *             codes beyond the matrix may hold anything.  scales, zeros: bf16 [ceil(rows/16)][ceil(K/group)][16], 16-byte
+ *             aligned like the codes; zeros NULL = 8.  More than 32 rows are computed 32 at a time, the weights read for each.
+ * KV8_APPEND  batch,tokens,n_kv,d,pos,cap,block  k,v,[positions(i32)],scales / kcodes,vcodes   ld0=row stride of k and v
+ *             k, v: rows b*tokens + t (bf16, or fp32 with IN_F32), head h at columns h*d; d = 64 or 128.  Token t of sequence b
+ *             becomes position p_b + t of the cache, p_b = positions[b] or pos; a sequence with a negative position takes no
+ *             part, tokens beyond the capacity are dropped.  The cache: kcodes, vcodes [batch,cap,n_kv,d] bytes (int8, e4m3 with
+ *             E4M3), scales fp32 [2][batch][ceil(cap/block)][n_kv] (keys', values'; written, although an input by place); a code
+ *             c stands for scale*c.  block: a multiple of 16 up to 1024.  A block's scale is the largest magnitude / 127 (e4m3:
+ *             / 448) of what is appended to it; if the block holds earlier positions and its scale is larger, that stays, and if
+ *             smaller, the earlier codes are rounded to the new one (code = round(code * old / new)).  Codes are round(x / scale),
+ *             to nearest even, in fp32 quotients.  A block that receives a NaN or an infinity reads as NaN.
+ * ATTN_DEC8   batch,n_q,n_kv,d,keys,cap,splits,block   q,kcodes,vcodes,[workspace],scales,[lens(i32)] / o   ld0=q row stride;
+ *             like ATTN_DEC, against KV8_APPEND's cache (E4M3 as there); 1 to 16 query heads per key/value head,    fparam0=scale
+ *             d = 64 or 128.  lens: keys of each sequence, at most `keys` (what is beyond counts as `keys`); a sequence of none
+ *             gets zeros.  Workspace and second step (ATTN_MERGE) as for ATTN_DEC; lithos_split_hint proposes splits.
+ * LOGPROBS    rows,vocab,top,splits              logits,[tokens(i32)],[workspace] / stats(f32),[ids(i32)]   ld0=of logits,
+ *             z = scale * logits (bf16, or fp32 with IN_F32; -infinity = not allowed); per row stats = log       ld1=of stats,
+ *             probability of tokens[row] (0 if that is outside the vocabulary or tokens is NULL), entropy, log-sum-  ld2=of ids;
+ *             exp, then the log probabilities of the `top` largest logits, their ids in ids; equal ones by the lower   fparam0=scale
+ *             id.  top <= 32.  A row without an allowed token: log-sum-exp and log probabilities -infinity, entropy 0; a
+ *             row with a NaN or +infinity: NaN, and any ids of the vocabulary.  splits > 1 cuts every row into ranges whose
+ *             partial results go to the workspace, rows*splits*(4 + 2 top) floats, and LOGPROBS_MERGE on the same queue joins them.
+ * LOGPROBS_MERGE rows,vocab,top,splits           logits,[tokens],workspace / stats,[ids]   as LOGPROBS
+ * LOGPROBS_GRAD rows,vocab                       logits,[tokens],stats,[g_logprob(f32)],[g_entropy(f32)] / dlogits   ld0=of logits,
+ *             dlogits = d(sum g_logprob*logprob + g_entropy*entropy) / d logits (bf16, fp32 with OUT_F32); stats are         ld1=of stats,
+ *             LOGPROBS's.  NULL gradients are zeros; rows without a given token take none from g_logprob.  May be in place.    ld2=of dlogits
  * RMSNORM     rows,H                             x,w(f32) / y                         fparam0=eps
  * ROPE_KV     rows,n_q,n_kv,d,pos,cap            qkv[rows,(n_q+2n_kv)d] (in place) / kcache,vcache   fparam0=theta
  *             qkv is bf16, or fp32 with IN_F32; the caches are always bf16 (rounded on append)
@@ -243,6 +283,11 @@ int lithos_op_grid(lithos_ctx_t* ctx, const lithos_op_t* op, lithos_dim3* grid_o
  * the flags of `op` are read; nothing is launched.  The caller then provides the fp32 planes
  * (slices * M * ldc floats) and follows the GEMM with SUM_SLICES. */
 int lithos_gemm_split_hint(const lithos_op_t* op, int32_t n_cus, int32_t* tile_out, int32_t* slices_out);
+
+/* Splits that put about two workgroups on each of `n_cus` compute units for an ATTN_DEC8 or a
+ * LOGPROBS descriptor (its own splits and workspace are not looked at); 1 = launch it whole.  The
+ * caller then provides the workspace and follows with ATTN_MERGE or LOGPROBS_MERGE. */
+int lithos_split_hint(const lithos_op_t* op, int32_t n_cus, int32_t* splits_out);
 
 /* Run `op` as ceil(total/atom_blocks) launches, atom i covering logical
  * blocks [i*atom_blocks, min((i+1)*atom_blocks, total)) of the grid numbered

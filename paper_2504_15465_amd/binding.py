@@ -20,9 +20,10 @@ OK, EINVAL, EHIP, EMASK, ESTATE, ELIMIT = 0, -1, -2, -3, -4, -5
 MASK_WORDS = 8
 MAX_SWEEP = 64
 
-OP_GEMM, OP_BIAS_ACT, OP_LAYERNORM, OP_SOFTMAX, OP_ATTN_ENC, OP_ATTN_DEC, OP_RMSNORM, OP_ROPE_KV, OP_SILU_MUL, OP_SPIN, OP_ATTN_MERGE, OP_SUM_SLICES, OP_ATTN_PREFILL = range(1, 14)
+OP_GEMM, OP_BIAS_ACT, OP_LAYERNORM, OP_SOFTMAX, OP_ATTN_ENC, OP_ATTN_DEC, OP_RMSNORM, OP_ROPE_KV, OP_SILU_MUL, OP_SPIN, OP_ATTN_MERGE, OP_SUM_SLICES, OP_ATTN_PREFILL, OP_GEMM_Q4, OP_KV8_APPEND, OP_ATTN_DEC8, OP_LOGPROBS, OP_LOGPROBS_MERGE, OP_LOGPROBS_GRAD = range(1, 20)
 ATTN_MAX_SPLITS = 64
-F_TRANS_A, F_TRANS_B, F_BIAS, F_GELU, F_RESIDUAL, F_OUT_F32, F_IN_F32, F_SPLIT_A, F_OUT_SPLIT, F_NORM_LN, F_NORM_RMS, F_GLU = (1 << i for i in range(12))
+LOGPROBS_MAX_SPLITS, LOGPROBS_MAX_TOP = 64, 32
+F_TRANS_A, F_TRANS_B, F_BIAS, F_GELU, F_RESIDUAL, F_OUT_F32, F_IN_F32, F_SPLIT_A, F_OUT_SPLIT, F_NORM_LN, F_NORM_RMS, F_GLU, F_E4M3 = (1 << i for i in range(13))
 TILE_AUTO, TILE_SKINNY, TILE_64, TILE_128, TILE_256 = 0, 1, 64, 128, 256
 MASK_STRIPED, MASK_WHOLE_XCD = 0, 1
 CLASS_HP, CLASS_BE = 0, 1
@@ -80,7 +81,7 @@ EXPORTS = [
     "lithos_init", "lithos_shutdown", "lithos_device_info", "lithos_last_error",
     "lithos_make_mask", "lithos_create_partition", "lithos_destroy_partition", "lithos_partition_cus",
     "lithos_partition_stream", "lithos_probe_partition", "lithos_partitions_coupled",
-    "lithos_op_grid", "lithos_gemm_split_hint", "lithos_launch_atomized", "lithos_launch_attn_dec_static",
+    "lithos_op_grid", "lithos_gemm_split_hint", "lithos_split_hint", "lithos_launch_atomized", "lithos_launch_attn_dec_static",
     "lithos_launch_atom", "lithos_partition_sync",
     "lithos_debug_block_counters", "lithos_rightsize", "lithos_time_launch",
     "lithos_tenant_create", "lithos_tenant_destroy", "lithos_submit", "lithos_sync_mark", "lithos_sync",
@@ -259,6 +260,65 @@ def attn_merge_op(workspace, o, batch, n_q, n_kv, d, splits, op_id=0) -> Op:
     return make_op(OP_ATTN_MERGE, (batch, n_q, n_kv, d, splits), flags, inputs=(workspace,), outputs=(o,), op_id=op_id)
 
 
+def gemm_q4_op(a, codes, scales, c, m, n, k, group, zeros=None, bias=None, gelu=False, residual=None, glu=False,
+               lda=None, ldc=None, ldr=None, op_id=0) -> Op:
+    """Weights in 4 bits as ``quant.pack_q4`` lays them out, ``scales`` and ``zeros`` (None: 8) as ``quant.pack_q4_groups`` does;
+    ``glu``: they have 2n rows, gate rows then up rows, and ``c`` = silu(gate product) * (up product)."""
+    flags = (F_BIAS if bias is not None else 0) | (F_GELU if gelu else 0) | (F_RESIDUAL if residual is not None else 0) | (F_GLU if glu else 0)
+    flags |= (F_IN_F32 if a.dtype == torch.float32 else 0) | (F_OUT_F32 if c.dtype == torch.float32 else 0)
+    return make_op(OP_GEMM_Q4, (m, n, k, group), flags,
+                   ld=(lda if lda is not None else k, 0, ldc if ldc is not None else n, ldr if ldr is not None else n),
+                   inputs=(a, codes, bias, residual, scales, zeros), outputs=(c,), op_id=op_id)
+
+
+def kv8_append_op(k, v, kcodes, vcodes, scales, batch, tokens, n_kv, d, pos, cap, block, positions=None, ldx=None, op_id=0) -> Op:
+    """Quantise ``tokens`` new keys and values per sequence into the cache, from position ``pos`` (or ``positions[b]``) on.
+    ``kcodes`` and ``vcodes`` are [batch, cap, n_kv, d] int8 or float8_e4m3fn, ``scales`` fp32 [2, batch, ceil(cap / block), n_kv]."""
+    flags = (F_IN_F32 if k.dtype == torch.float32 else 0) | (F_E4M3 if kcodes.dtype == torch.float8_e4m3fn else 0)
+    return make_op(OP_KV8_APPEND, (batch, tokens, n_kv, d, pos, cap, block), flags, ld=(ldx if ldx is not None else n_kv * d,),
+                   inputs=(k, v, positions, scales), outputs=(kcodes, vcodes), op_id=op_id)
+
+
+def attn_dec8_op(q, kcodes, vcodes, scales, o, batch, n_q, n_kv, d, keys, cap, block, scale, lens=None, ldq=None, op_id=0,
+                 splits=1, workspace=None) -> Op:
+    """Decode attention against a cache of ``kv8_append_op``; ``lens``: int32 keys per sequence (None: ``keys`` everywhere).
+    splits > 1 needs an fp32 workspace of attn_workspace_floats(...) elements and an attn_merge_op after it."""
+    flags = (F_IN_F32 if q.dtype == torch.float32 else 0) | (F_OUT_F32 if o.dtype == torch.float32 else 0)
+    flags |= F_E4M3 if kcodes.dtype == torch.float8_e4m3fn else 0
+    return make_op(OP_ATTN_DEC8, (batch, n_q, n_kv, d, keys, cap, splits, block), flags, ld=(ldq if ldq is not None else n_q * d,),
+                   fparam=(scale,), inputs=(q, kcodes, vcodes, workspace, scales, lens), outputs=(o,), op_id=op_id)
+
+
+def logprobs_workspace_floats(rows, top, splits) -> int:
+    return rows * splits * (4 + 2 * top)
+
+
+def _logprobs(kind, logits, tokens, stats, ids, rows, vocab, top, splits, workspace, scale, ldx, lds, ldi, op_id) -> Op:
+    return make_op(kind, (rows, vocab, top, splits), F_IN_F32 if logits.dtype == torch.float32 else 0,
+                   ld=(ldx if ldx is not None else vocab, lds if lds is not None else 3 + top, ldi if ldi is not None else top),
+                   fparam=(scale,), inputs=(logits, tokens, workspace), outputs=(stats, ids), op_id=op_id)
+
+
+def logprobs_op(logits, tokens, stats, ids, rows, vocab, top=0, scale=1.0, ldx=None, lds=None, ldi=None, splits=1, workspace=None, op_id=0) -> Op:
+    """``stats`` fp32 [rows, 3 + top]: log probability of ``tokens`` (int32, None: none), entropy, log-sum-exp, top log probabilities;
+    ``ids`` int32 [rows, top].  splits > 1 needs an fp32 workspace of logprobs_workspace_floats(...) elements and a
+    logprobs_merge_op after it."""
+    return _logprobs(OP_LOGPROBS, logits, tokens, stats, ids, rows, vocab, top, splits, workspace, scale, ldx, lds, ldi, op_id)
+
+
+def logprobs_merge_op(workspace, logits, tokens, stats, ids, rows, vocab, top, splits, scale=1.0, ldx=None, lds=None, ldi=None, op_id=0) -> Op:
+    """Second step of a split ``logprobs_op``, whose other arguments it repeats."""
+    return _logprobs(OP_LOGPROBS_MERGE, logits, tokens, stats, ids, rows, vocab, top, splits, workspace, scale, ldx, lds, ldi, op_id)
+
+
+def logprobs_grad_op(logits, tokens, stats, g_logprob, g_entropy, dlogits, rows, vocab, scale=1.0, ldx=None, lds=None, ldd=None, op_id=0) -> Op:
+    """Gradient of sum(g_logprob * log probability + g_entropy * entropy) with respect to the logits (None: zeros)."""
+    flags = (F_IN_F32 if logits.dtype == torch.float32 else 0) | (F_OUT_F32 if dlogits.dtype == torch.float32 else 0)
+    lds = lds if lds is not None else stats.shape[-1]
+    return make_op(OP_LOGPROBS_GRAD, (rows, vocab), flags, ld=(ldx if ldx is not None else vocab, lds, ldd if ldd is not None else vocab),
+                   fparam=(scale,), inputs=(logits, tokens, stats, g_logprob, g_entropy), outputs=(dlogits,), op_id=op_id)
+
+
 def spin_op(blocks, ticks, op_id=0) -> Op:
     return make_op(OP_SPIN, (blocks, ticks), op_id=op_id)
 
@@ -338,6 +398,13 @@ def lithos_gemm_split_hint(op: Op, n_cus=256):
     tile, slices = C.c_int32(0), C.c_int32(0)
     _check(lib().lithos_gemm_split_hint(C.byref(op), int(n_cus), C.byref(tile), C.byref(slices)))
     return tile.value, slices.value
+
+
+def lithos_split_hint(op: Op, n_cus=256) -> int:
+    """Splits that fill ``n_cus`` compute units with an ATTN_DEC8 or LOGPROBS descriptor; 1: launch it whole."""
+    splits = C.c_int32(0)
+    _check(lib().lithos_split_hint(C.byref(op), int(n_cus), C.byref(splits)))
+    return splits.value
 
 
 def lithos_launch_atomized(ctx, op: Op, grid=(0, 0, 0), atom_blocks=0, part=None, stream=None):

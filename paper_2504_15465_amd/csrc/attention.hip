@@ -360,14 +360,13 @@ __global__ __launch_bounds__(256, 3) void attn_dec_kernel(AttnArgs a, AtomArgs a
     }
 }
 
-// Merge of the splits' partial softmaxes, in split order.  One workgroup per
-// (sequence, key/value head).
-template <int G, bool O32>
+// Merge of the splits' partial softmaxes, in split order (ATTN_DEC's and ATTN_DEC8's, whose
+// workspaces are alike).  One workgroup per (sequence, key/value head).
+template <int D, bool O32>
 __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a, AtomArgs atom)
 {
-    constexpr int D = 128;
     const uint32_t bg = atom_logical_block(atom);
-    const int b = bg / a.n_kv, g = bg % a.n_kv, S = a.splits;
+    const int b = bg / a.n_kv, g = bg % a.n_kv, S = a.splits, G = a.n_q / a.n_kv;
     const float* ws = a.ws;
     const float* ml = ws + (int64_t)a.batch * a.n_kv * S * G * D;
     for (int i = threadIdx.x; i < G * D; i += 256) {
@@ -384,6 +383,7 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a, AtomArgs at
 #pragma unroll
             for (int u = 0; u < 8; ++u) gm = fmaxf(gm, m8[u]);
         }
+        const float ref = gm == -INFINITY ? 0.0f : gm;                      // a sequence without keys (ATTN_DEC8)
         float num = 0.0f, den = 0.0f;
         for (int s0 = 0; s0 < S; s0 += 8) {
             float2 p8[8];
@@ -396,12 +396,12 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a, AtomArgs at
             }
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const float f = s0 + u < S ? expf(p8[u].x - gm) : 0.0f;     // 0 for a split without keys
+                const float f = s0 + u < S ? expf(p8[u].x - ref) : 0.0f;    // 0 for a split without keys
                 num += o8[u] * f;
                 den += p8[u].y * f;
             }
         }
-        const float r = num / den;
+        const float r = den == 0.0f ? 0.0f : num / den;
         const int64_t idx = (int64_t)b * ((int64_t)a.n_q * D) + (g * G + h) * D + d;
         if constexpr (O32) reinterpret_cast<float*>(a.o)[idx] = r;
         else reinterpret_cast<uint16_t*>(a.o)[idx] = f32_to_bf16(r);
@@ -432,9 +432,8 @@ static attn_fn attn_kernel(const lithos_op_t& op)
     const int G = (int)(op.dim[1] / op.dim[2]);
     const bool o32 = op.flags & LITHOS_F_OUT_F32;
     if (op.kind == LITHOS_OP_ATTN_MERGE)
-        return G == 1 ? (o32 ? (attn_fn)attn_merge_kernel<1, true> : (attn_fn)attn_merge_kernel<1, false>)
-             : G == 2 ? (o32 ? (attn_fn)attn_merge_kernel<2, true> : (attn_fn)attn_merge_kernel<2, false>)
-                      : (o32 ? (attn_fn)attn_merge_kernel<4, true> : (attn_fn)attn_merge_kernel<4, false>);
+        return op.dim[3] == 64 ? (o32 ? (attn_fn)attn_merge_kernel<64, true> : (attn_fn)attn_merge_kernel<64, false>)
+                               : (o32 ? (attn_fn)attn_merge_kernel<128, true> : (attn_fn)attn_merge_kernel<128, false>);
     return dec_fn(G, op.flags & LITHOS_F_IN_F32, o32);
 }
 
@@ -466,8 +465,8 @@ int attn_plan(const lithos_op_t& op, OpPlan* plan)
         const int64_t batch = op.dim[0], n_q = op.dim[1], n_kv = op.dim[2], d = op.dim[3], splits = op.dim[4];
         if (batch <= 0 || n_q <= 0 || n_kv <= 0 || n_q % n_kv || batch * n_kv > 0x7fffffff) return fail(LITHOS_EINVAL, "attn_merge: need batch > 0 and n_kv dividing n_q");
         const int64_t G = n_q / n_kv;
-        if (G != 1 && G != 2 && G != 4) return fail(LITHOS_EINVAL, "attn_merge: group size %lld is not built (1, 2, 4)", (long long)G);
-        if (d != 128) return fail(LITHOS_EINVAL, "attn_merge: head width %lld is not built (128 only)", (long long)d);
+        if (G > 16) return fail(LITHOS_EINVAL, "attn_merge: group size %lld is not built (1 to 16)", (long long)G);
+        if (d != 64 && d != 128) return fail(LITHOS_EINVAL, "attn_merge: head width %lld is not built (64, 128)", (long long)d);
         if (splits < 1 || splits > LITHOS_ATTN_MAX_SPLITS) return fail(LITHOS_EINVAL, "attn_merge: splits %lld outside 1..%d", (long long)splits, LITHOS_ATTN_MAX_SPLITS);
         if (!op.in[0] || !op.out[0]) return fail(LITHOS_EINVAL, "attn_merge: null operand");
         plan->grid = {(uint32_t)n_kv, (uint32_t)batch, 1};

@@ -46,6 +46,14 @@ int attn_plan(const lithos_op_t& op, OpPlan* plan);
 int attn_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& atom, hipStream_t s);
 int attn_prefill_plan(const lithos_op_t& op, OpPlan* plan);
 int attn_prefill_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& atom, hipStream_t s);
+int kv8_plan(const lithos_op_t& op, OpPlan* plan);               // KV8_APPEND, ATTN_DEC8
+int kv8_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& atom, hipStream_t s);
+int kv8_split_hint(const lithos_op_t& op, int n_cus);
+int gemm_q4_plan(const lithos_op_t& op, OpPlan* plan);
+int gemm_q4_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& atom, hipStream_t s);
+int logprobs_plan(const lithos_op_t& op, OpPlan* plan);          // LOGPROBS, LOGPROBS_MERGE, LOGPROBS_GRAD
+int logprobs_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& atom, hipStream_t s);
+int logprobs_split_hint(const lithos_op_t& op, int n_cus);
 int spin_plan(const lithos_op_t& op, OpPlan* plan);
 int spin_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& atom, hipStream_t s);
 int probe_launch(uint32_t n_wg, uint32_t* dev_xcd, uint32_t* dev_hwid, hipStream_t s);
@@ -136,5 +144,6 @@ __device__ __forceinline__ float gelu_erf(float u)
 }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned_to(const void* p, unsigned bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }      // null is
 
 } // namespace lithos

@@ -101,6 +101,12 @@ int op_plan(const lithos_op_t& op, OpPlan* plan)
     case LITHOS_OP_ATTN_MERGE:
     case LITHOS_OP_ATTN_DEC: return attn_plan(op, plan);
     case LITHOS_OP_ATTN_PREFILL: return attn_prefill_plan(op, plan);
+    case LITHOS_OP_GEMM_Q4: return gemm_q4_plan(op, plan);
+    case LITHOS_OP_KV8_APPEND:
+    case LITHOS_OP_ATTN_DEC8: return kv8_plan(op, plan);
+    case LITHOS_OP_LOGPROBS:
+    case LITHOS_OP_LOGPROBS_MERGE:
+    case LITHOS_OP_LOGPROBS_GRAD: return logprobs_plan(op, plan);
     case LITHOS_OP_BIAS_ACT:
     case LITHOS_OP_LAYERNORM:
     case LITHOS_OP_SOFTMAX:
@@ -122,6 +128,12 @@ int op_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& atom, h
     case LITHOS_OP_ATTN_MERGE:
     case LITHOS_OP_ATTN_DEC: return attn_launch(op, plan, atom, s);
     case LITHOS_OP_ATTN_PREFILL: return attn_prefill_launch(op, plan, atom, s);
+    case LITHOS_OP_GEMM_Q4: return gemm_q4_launch(op, plan, atom, s);
+    case LITHOS_OP_KV8_APPEND:
+    case LITHOS_OP_ATTN_DEC8: return kv8_launch(op, plan, atom, s);
+    case LITHOS_OP_LOGPROBS:
+    case LITHOS_OP_LOGPROBS_MERGE:
+    case LITHOS_OP_LOGPROBS_GRAD: return logprobs_launch(op, plan, atom, s);
     default: return rowops_launch(op, plan, atom, s);
     }
 }
@@ -454,6 +466,19 @@ int lithos_gemm_split_hint(const lithos_op_t* op, int32_t n_cus, int32_t* tile_o
     if (s > kt / 8) s = kt / 8;
     if (s > LITHOS_GEMM_MAX_SLICES) s = LITHOS_GEMM_MAX_SLICES;
     if (s >= 2) { *tile_out = LITHOS_TILE_256; *slices_out = (int32_t)s; }
+    return LITHOS_OK;
+}
+
+int lithos_split_hint(const lithos_op_t* op, int32_t n_cus, int32_t* splits_out)
+{
+    if (!op || !splits_out || n_cus <= 0 || (op->kind != LITHOS_OP_ATTN_DEC8 && op->kind != LITHOS_OP_LOGPROBS))
+        return fail(LITHOS_EINVAL, "lithos_split_hint: need an ATTN_DEC8 or LOGPROBS descriptor, a CU count and an output");
+    lithos_op_t whole = *op;
+    whole.dim[op->kind == LITHOS_OP_ATTN_DEC8 ? 6 : 3] = 1;
+    OpPlan plan;
+    const int rc = op_plan(whole, &plan);
+    if (rc != LITHOS_OK) return rc;
+    *splits_out = op->kind == LITHOS_OP_ATTN_DEC8 ? kv8_split_hint(whole, n_cus) : logprobs_split_hint(whole, n_cus);
     return LITHOS_OK;
 }
 
