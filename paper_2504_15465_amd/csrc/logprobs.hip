@@ -7,9 +7,11 @@
 //   lse = c m + log l,   H = log l - t / l;   when m rises by r (in units of d): t <- f (t - l r), l <- f l, f = exp(-r).
 // Each lane keeps (m, l, t) of its own elements; lanes, wavefronts and splits are joined in a fixed order.
 //
-// The most likely tokens: a wavefront keeps a list of up to `top` keys (value, index) in LDS.  Elements above its
-// smallest value are rare once it is full; they are gathered behind it and the list is chosen anew when 64 wait.  The
-// first tile fills the list: the top-th of the 64 lanes' largest keys is a bound below which nothing can be chosen.
+// The most likely tokens: every lane notes the largest of its elements in each of up to eight stretches.  If m of the four
+// wavefronts have j lanes each, m j >= top, whose largest element reaches a bound, so do `top` elements, all of them in the
+// few stretches whose largest does; the bound is the best for m = 4, 2 and 1.  The elements of these stretches are read a
+// second time; those that reach the bound find their places by counting larger ones.  (A list kept during the pass cost
+// more: 2048 rows of 131072 bf16 took 132 us with top = 5 and 171 with 32, against 105 without tokens.)
 // Bound by the bytes of the logits, read once.
 #include "common.hpp"
 #include <math.h>
@@ -28,7 +30,12 @@ struct LogprobArgs {
     float scale;
 };
 
-constexpr int LP_TOP = LITHOS_LOGPROBS_MAX_TOP, LP_WAIT = 128;
+constexpr int LP_TOP = LITHOS_LOGPROBS_MAX_TOP, LP_ROOM = 2048, LP_SEG = 8;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4_b4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_b2 __attribute__((ext_vector_type(4), aligned(2)));
+
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 // larger key = larger value, then lower index; -0 is 0
@@ -70,24 +77,29 @@ __device__ __forceinline__ Soft soft_wave(Soft s, float c2)
     return s;
 }
 
-// The k largest of n keys (n <= 64 * PER), sorted, at out[0 .. min(k, n)); keys are distinct.  One wavefront.
-template <int PER>
-__device__ __forceinline__ void choose_top(const uint64_t* keys, int n, int k, uint64_t* out, int lane)
+// one lane's key, the same in every lane
+__device__ __forceinline__ uint64_t key_of_lane(uint64_t k, int lane)
 {
-    uint64_t mine[PER];
-    int above[PER];
+    return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
+}
+
+// The k largest of n distinct keys in LDS, sorted, to `out`: a key's place is the number of larger ones.  By the whole
+// workgroup; the caller puts barriers around it.
+__device__ __forceinline__ void choose_top(const uint64_t* keys, int n, int k, uint64_t* out)
+{
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const uint64_t mine = keys[i];
+        int above = 0, o = 0;
+        for (; o + 8 <= n; o += 8) {
+            uint64_t other[8];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) { mine[i] = i * 64 + lane < n ? keys[i * 64 + lane] : 0; above[i] = 0; }
-    for (int j = 0; j < n; ++j) {
-        const uint64_t o = keys[j];
+            for (int u = 0; u < 8; ++u) other[u] = keys[o + u];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) above[i] += o > mine[i];
+            for (int u = 0; u < 8; ++u) above += other[u] > mine;
+        }
+        for (; o < n; ++o) above += keys[o] > mine;
+        if (above < k) out[above] = mine;
     }
-    wave_lds_sync();                             // `out` may overlap `keys`
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if (i * 64 + lane < n && above[i] < k) out[above[i]] = mine[i];
-    wave_lds_sync();
 }
 
 // what is written of a row
@@ -122,93 +134,88 @@ __device__ __forceinline__ int given_token(const LogprobArgs& a, int64_t row)
     return (uint32_t)t < (uint32_t)a.vocab ? t : -1;
 }
 
-typedef float f32x4_b4 __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32x4_b2 __attribute__((ext_vector_type(4), aligned(2)));
 
 // Logical block = (row, split).  The split's elements are tiles of 1024 which its four wavefronts take in turn; a lane
 // owns 16 of a tile, in runs of 4 (fp32) or 8 (bf16).
 template <bool X32>
 __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs atom)
 {
-    constexpr int RUN = X32 ? 4 : 8, TILE = 1024;
-    __shared__ uint64_t keys[4][LP_TOP + LP_WAIT];
+    constexpr int RUN = X32 ? 4 : 8, TILE = 1024, NW = X32 ? 16 : 8;      // NW dwords of a tile per lane
+    __shared__ __attribute__((aligned(16))) uint64_t cand[LP_ROOM + LP_TOP];
+    __shared__ uint64_t chosen[LP_TOP];
     __shared__ Soft softs[4];
-    __shared__ int counts[4];
+    __shared__ float nth[3][4];                   // per wavefront: its ceil(K / 4)-th, ceil(K / 2)-th and K-th largest lane maximum
+    __shared__ float peaks[LP_SEG][256];          // largest elements of the lanes' stretches
+    __shared__ uint16_t sel[LP_SEG * 256];
+    __shared__ int n_sel, n_cand;
 
     const uint32_t L = atom_logical_block(atom);
     const int64_t row = L / a.splits;
     const int sp = L % a.splits;
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tiles = (a.vocab + TILE - 1) / TILE;
     const int t0 = (int)((int64_t)sp * tiles / a.splits), t1 = (int)((int64_t)(sp + 1) * tiles / a.splits);
     const float c2 = a.scale * LOG2E;
     const int K = a.top;
 
     const char* const xrow = reinterpret_cast<const char*>(a.x) + row * a.ldx * (X32 ? 4 : 2);
-    auto index = [&](int tile, int e) { return tile * TILE + (e / RUN) * 64 * RUN + lane * RUN + e % RUN; };
-    auto load = [&](int tile, float (&x)[16]) {
-        if ((tile + 1) * TILE <= a.vocab) {
-            if constexpr (X32) {
+    // element e of lane l; the last, partial tile is dealt out one element after another, so that every lane has some
+    auto index = [&](int tile, int l, int e) { return tile * TILE + ((tile + 1) * TILE <= a.vocab ? (e / RUN) * 64 * RUN + l * RUN + e % RUN : e * 64 + l); };
+    // elements RUN q .. RUN q + RUN - 1 of lane l as four dwords
+    auto load = [&](int tile, int l, int q) {
+        if ((tile + 1) * TILE <= a.vocab) return u32x4(*reinterpret_cast<const u32x4_b2*>(xrow + (int64_t)index(tile, l, RUN * q) * (X32 ? 4 : 2)));
+        uint32_t one[RUN];                       // what lies beyond the row is -infinity
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const f32x4_b4 v = *reinterpret_cast<const f32x4_b4*>(xrow + (int64_t)index(tile, 4 * q) * 4);
+        for (int e = 0; e < RUN; ++e) {
+            const int at = min(index(tile, l, RUN * q + e), a.vocab - 1);
+            if constexpr (X32) one[e] = reinterpret_cast<const uint32_t*>(xrow)[at];
+            else one[e] = reinterpret_cast<const uint16_t*>(xrow)[at];
+        }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[4 * q + e] = v[e];
-                }
-            } else {
+        for (int e = 0; e < RUN; ++e) if (index(tile, l, RUN * q + e) >= a.vocab) one[e] = X32 ? 0xff800000u : 0xff80u;
+        u32x4 v;
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const u32x4_b2 v = *reinterpret_cast<const u32x4_b2*>(xrow + (int64_t)index(tile, 8 * q) * 2);
+        for (int d = 0; d < 4; ++d) v[d] = X32 ? one[d] : one[(2 * d) % RUN] | (one[(2 * d + 1) % RUN] << 16);
+        return v;
+    };
+    auto unpack = [&](const u32x4& v, float* x) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { x[8 * q + 2 * e] = __uint_as_float(v[e] << 16); x[8 * q + 2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u); }
-                }
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = index(tile, e);
-                x[e] = i < a.vocab ? logit_at<X32>(a, row, i) : -INFINITY;
-            }
+        for (int d = 0; d < 4; ++d) {
+            if constexpr (X32) x[d] = __uint_as_float(v[d]);
+            else { x[2 * d] = __uint_as_float(v[d] << 16); x[2 * d + 1] = __uint_as_float(v[d] & 0xffff0000u); }
         }
     };
 
-    Soft s = {-INFINITY, 0.0f, 0.0f};
-    uint64_t* const list = keys[wave];
-    int have = 0, wait = 0;                       // keys chosen, keys waiting behind place LP_TOP
-    uint64_t least_key = 0;                       // smallest key chosen, once K are, and its value
-    float least = -INFINITY;
-    auto choose = [&]() {
-        // chosen keys first, waiting ones behind them without a gap
-        uint64_t moved[2];
+    Soft s = {-INFINITY, 0.0f, 0.0f};            // m: a value near the largest one, see below
+    float most = -INFINITY, peak = -INFINITY;     // the largest of this lane's elements, of its present stretch
+    const int turns = (t1 - t0 + 3) / 4, len = max(1, (turns + LP_SEG - 1) / LP_SEG);
+    int left = len, seg = 0;
+    u32x4 raw[NW / 4];
+    if (t0 + wave < t1)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) moved[i] = i * 64 + lane < wait ? list[LP_TOP + i * 64 + lane] : 0;
-        wave_lds_sync();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) if (i * 64 + lane < wait) list[have + i * 64 + lane] = moved[i];
-        wave_lds_sync();
-        choose_top<3>(list, have + wait, K, list, lane);
-        have = min(K, have + wait);
-        wait = 0;
-        if (have == K) { least_key = list[K - 1]; least = key_value(least_key); }
-    };
-    auto gather = [&](bool mine, uint64_t key) {
-        const uint64_t all = __ballot(mine);
-        if (all == 0) return;
-        if (mine) list[LP_TOP + wait + __popcll(all & ((1ull << lane) - 1))] = key;
-        wait += __popcll(all);
-        wave_lds_sync();
-        if (wait > LP_WAIT - 64) choose();
-    };
-
-    bool first = true;
+        for (int q = 0; q < NW / 4; ++q) raw[q] = load(t0 + wave, lane, q);
     for (int tile = t0 + wave; tile < t1; tile += 4) {
         float x[16];
-        load(tile, x);
+#pragma unroll
+        for (int q = 0; q < NW / 4; ++q) unpack(raw[q], x + RUN * q);
+        if (tile + 4 < t1)
+#pragma unroll
+            for (int q = 0; q < NW / 4; ++q) raw[q] = load(tile + 4, lane, q);
+
         float mt = x[0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) mt = fmaxf(mt, x[e]);
-        if (__any(mt > s.m)) {
+        peak = fmaxf(peak, mt);
+        if (--left == 0 || tile + 4 >= t1) {                    // the stretch ends
+            if (K) peaks[seg][tid] = peak;
+            most = fmaxf(most, peak);
+            peak = -INFINITY;
+            left = len;
+            ++seg;
+        }
+        // the sums' reference follows the largest value once that is 2^8 times as likely
+        if (__any(s.m == -INFINITY ? mt > s.m : (mt - s.m) * c2 > 8.0f)) {
             const float nm = fmaxf(s.m, mt), ref = nm == -INFINITY ? 0.0f : nm;
             const float r = fmaxf((s.m - ref) * c2, -300.0f), f = __builtin_amdgcn_exp2f(r);
             s.t = f * fmaf(r, s.l, s.t);
@@ -223,97 +230,159 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
             s.l += p;
             s.t = fmaf(p, fmaxf(d, -300.0f), s.t);            // 0, not infinity times 0, for a forbidden token
         }
-        if (K == 0) continue;
-        if (first) {
-            first = false;
-            uint64_t best = 0;
+    }
+
+    if (K) {
+        int above = 0;
+#pragma unroll 8
+        for (int o = 0; o < 64; ++o) above += __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(most), o)) > most;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = index(tile, e);
-                const uint64_t k = top_key(x[e], i);
-                if (i < a.vocab && k > best) best = k;
-            }
-            int above = 0;
-            for (int j = 0; j < 64; ++j) above += __shfl(best, j) > best;
-            // the K-th largest of the lanes' best keys (0, of a lane without elements, if there are not as many)
-            const uint64_t at = __ballot(above == K - 1 && best != 0);
-            const uint64_t bound = at ? __shfl(best, __ffsll((unsigned long long)at) - 1) : 1;
+        for (int i = 0; i < 3; ++i) {
+            // of the maxima that fewer than j lanes exceed the least one: with equal ones it is exceeded by fewer than j - 1
+            int c = (K + (4 >> i) - 1) / (4 >> i) - 1;
+            uint64_t at;
+            while ((at = __ballot(above == c)) == 0) --c;
+            if (lane == 0) nth[i][wave] = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(most), __ffsll((unsigned long long)at) - 1));
+        }
+        if (tid == 0) n_sel = n_cand = 0;
+    }
+    s = soft_wave(s, c2);
+    if (lane == 0) softs[wave] = s;
+    __syncthreads();
+    if (K) {
+        const float lo01 = fminf(nth[1][0], nth[1][1]), hi01 = fmaxf(nth[1][0], nth[1][1]), lo23 = fminf(nth[1][2], nth[1][3]), hi23 = fmaxf(nth[1][2], nth[1][3]);
+        float bound = fminf(fminf(nth[0][0], nth[0][1]), fminf(nth[0][2], nth[0][3]));
+        bound = fmaxf(bound, fmaxf(fminf(hi01, hi23), fmaxf(lo01, lo23)));                 // second largest
+        bound = fmaxf(bound, fmaxf(fmaxf(nth[2][0], nth[2][1]), fmaxf(nth[2][2], nth[2][3])));
+        for (int g = 0; g < seg; ++g) {
+            const float p = peaks[g][tid];
+            if (p >= bound && p > -INFINITY) sel[atomicAdd(&n_sel, 1)] = (uint16_t)(g * 256 + tid);     // in any order, as below: places follow from keys
+        }
+        __syncthreads();
+        constexpr int RUNS = 16 / RUN;
+        const int ns = n_sel, items = ns * len * RUNS;
+        // elements above `floor` (a key) of item i, a run of a stretch, to the candidates
+        auto scan = [&](int i, uint64_t floor) {
+            const int who = sel[i / (RUNS * len)] & 255, g = sel[i / (RUNS * len)] >> 8, q = i % RUNS, tile = t0 + (who >> 6) + 4 * (g * len + i / RUNS % len);
+            if (tile >= t1) return;
+            float x[RUN];
+            unpack(load(tile, who & 63, q), x);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = index(tile, e);
-                const uint64_t k = top_key(x[e], i);
-                gather(i < a.vocab && k >= bound, k);
-            }
-            choose();
-        } else if (have < K || __any(mt > least)) {           // an equal value of a later tile has a higher index
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = index(tile, e);
-                const uint64_t k = top_key(x[e], i);
-                gather(i < a.vocab && k > least_key, k);
+            for (int e = 0; e < RUN; ++e)
+                if (x[e] >= bound && x[e] > -INFINITY) {
+                    const uint64_t k = top_key(x[e], index(tile, who & 63, RUN * q + e));
+                    if (k > floor) {
+                        const int at = atomicAdd(&n_cand, 1);
+                        if (at < LP_ROOM + LP_TOP) cand[at] = k;
+                    }
+                }
+        };
+        // of forbidden tokens, where fewer than K are allowed, the first K suffice
+        auto fill = [&]() {
+            const int i = t0 * TILE + tid;
+            if (bound == -INFINITY && tid < K && i < min(t1 * TILE, a.vocab) && logit_at<X32>(a, row, i) == -INFINITY) cand[atomicAdd(&n_cand, 1)] = top_key(-INFINITY, i);
+        };
+        fill();
+        for (int i = tid; i < items; i += 256) scan(i, 0);
+        __syncthreads();
+        int n = n_cand;
+        if (n > LP_ROOM) {
+            // many equal values: 256 items at a time, and only what is above the K-th chosen so far
+            __syncthreads();
+            if (tid == 0) n_cand = 0;
+            __syncthreads();
+            fill();
+            n = 0;
+            for (int i0 = 0; i0 < items; i0 += 256) {
+                if (i0 + tid < items) scan(i0 + tid, n >= K ? chosen[K - 1] : 0);
+                __syncthreads();
+                n = n_cand;
+                choose_top(cand, n, K, chosen);
+                __syncthreads();
+                n = min(n, K);
+                if (tid < n) cand[tid] = chosen[tid];
+                if (tid == 0) n_cand = n;
+                __syncthreads();
             }
         }
+        __syncthreads();
+        choose_top(cand, n, K, chosen);
+        __syncthreads();
+        n = min(n, K);
+        if (a.splits == 1 && tid >= n && tid < K) chosen[tid] = top_key(-INFINITY, tid);      // rows with NaN: any token
+        if (wave == 0 && a.splits > 1) {
+            float* w = a.ws + ((int64_t)row * a.splits + sp) * (4 + 2 * K);
+            if (lane == 0) w[3] = (float)n;
+            if (lane < n) reinterpret_cast<uint2*>(w + 4)[lane] = make_uint2((uint32_t)chosen[lane], (uint32_t)(chosen[lane] >> 32));
+        }
     }
-    if (wait) choose();
-    s = soft_wave(s, c2);
-    if (lane == 0) { softs[wave] = s; counts[wave] = have; }
-    __syncthreads();
     if (wave != 0) return;
-
     s = softs[0];
 #pragma unroll
     for (int w = 1; w < 4; ++w) s = soft_join(s, softs[w], c2);
-    // the four lists, one after another, in the first two wavefronts' room
-    uint64_t* const all = keys[0];
-    int n = counts[0];
-    for (int w = 1; w < 4; ++w) {
-        const uint64_t k = lane < counts[w] ? keys[w][lane] : 0;
-        wave_lds_sync();
-        if (lane < counts[w]) all[n + lane] = k;
-        wave_lds_sync();
-        n += counts[w];
-    }
-    choose_top<2>(all, n, K, all, lane);
-    n = min(n, K);
     if (a.splits == 1) {
         const int t = given_token(a, row);
-        write_row(a, row, s, t >= 0 ? logit_at<X32>(a, row, t) : 0.0f, t >= 0, all, lane);
-    } else {
+        wave_lds_sync();
+        write_row(a, row, s, t >= 0 ? logit_at<X32>(a, row, t) : 0.0f, t >= 0, chosen, lane);
+    } else if (lane == 0) {
         float* w = a.ws + ((int64_t)row * a.splits + sp) * (4 + 2 * K);
-        if (lane == 0) { w[0] = s.m; w[1] = s.l; w[2] = s.t; w[3] = (float)n; }
-        if (lane < n) reinterpret_cast<uint2*>(w + 4)[lane] = make_uint2((uint32_t)all[lane], (uint32_t)(all[lane] >> 32));
+        w[0] = s.m; w[1] = s.l; w[2] = s.t;
+        if (K == 0) w[3] = 0.0f;
     }
 }
 
-// Joins the splits of a row, in split order.  One workgroup of one wavefront's work per row; four rows per workgroup.
+// Joins the splits of a row: one workgroup per row.  With j = ceil(top / splits) at least `top` keys are as large as the
+// ceil(top / j)-th largest of the splits' j-th keys; the few that are find their places by counting larger ones.
 template <bool X32>
 __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobArgs a, AtomArgs atom)
 {
-    __shared__ uint64_t keys[4][3 * 64];
-    const uint32_t L = atom_logical_block(atom);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = (int64_t)L * 4 + wave;
-    if (row >= a.rows) return;
+    __shared__ __attribute__((aligned(16))) uint64_t cand[LITHOS_LOGPROBS_MAX_SPLITS * LP_TOP + 1];
+    __shared__ uint64_t chosen[LP_TOP], bound_s;
+    __shared__ int n_cand;
+    const int64_t row = atom_logical_block(atom);
+    const int tid = threadIdx.x, lane = tid & 63;
     const float c2 = a.scale * LOG2E;
-    const int K = a.top;
+    const int K = a.top, S = a.splits, stride = 4 + 2 * K;
+    const float* const ws = a.ws + row * S * stride;
+    auto key_at = [&](int sp, int j) {
+        const uint2 k = reinterpret_cast<const uint2*>(ws + sp * stride + 4)[j];
+        return ((uint64_t)k.y << 32) | k.x;
+    };
     Soft s = {-INFINITY, 0.0f, 0.0f};
-    uint64_t* const list = keys[wave];
-    int n = 0;
-    for (int sp = 0; sp < a.splits; ++sp) {
-        const float* w = a.ws + (row * a.splits + sp) * (4 + 2 * K);
-        s = soft_join(s, Soft{w[0], w[1], w[2]}, c2);
-        const int more = (int)w[3];
-        if (lane < more) {
-            const uint2 k = reinterpret_cast<const uint2*>(w + 4)[lane];
-            list[n + lane] = ((uint64_t)k.y << 32) | k.x;
-        }
-        n += more;
-        wave_lds_sync();
-        if (n > 3 * 64 - LP_TOP) { choose_top<3>(list, n, K, list, lane); n = K; }
-    }
-    choose_top<3>(list, n, K, list, lane);
     const int t = given_token(a, row);
-    write_row(a, row, s, t >= 0 ? logit_at<X32>(a, row, t) : 0.0f, t >= 0, list, lane);
+    float logit = 0.0f;
+    if (tid < 64) {
+        if (t >= 0) logit = logit_at<X32>(a, row, t);
+        const f32x4_b4 p = lane < S ? *reinterpret_cast<const f32x4_b4*>(ws + lane * stride) : f32x4_b4{-INFINITY, 0.0f, 0.0f, 0.0f};
+        if (K) {
+            const int j = (K + S - 1) / S, m = (K + j - 1) / j;
+            const uint64_t mine = lane < S && (int)p.w >= j ? key_at(lane, j - 1) : 0;
+            int above = 0;
+#pragma unroll 8
+            for (int o = 0; o < 64; ++o) above += key_of_lane(mine, o) > mine;
+            const uint64_t at = __ballot(above == m - 1 && mine != 0);
+            if (lane == 0) { n_cand = 0; bound_s = 0; }
+            if (at && lane == __ffsll((unsigned long long)at) - 1) bound_s = mine;
+        }
+        s = soft_wave(Soft{p.x, p.y, p.z}, c2);
+    }
+    if (K) {
+        __syncthreads();
+        const uint64_t bound = bound_s;
+        for (int i = tid; i < S * K; i += 256) {
+            const int sp = i / K, j = i % K;
+            if (j < (int)ws[sp * stride + 3]) {
+                const uint64_t k = key_at(sp, j);
+                if (k >= bound) cand[atomicAdd(&n_cand, 1)] = k;        // in any order: places follow from the keys
+            }
+        }
+        __syncthreads();
+        const int n = n_cand;
+        choose_top(cand, n, K, chosen);
+        if (tid >= n && tid < K) chosen[tid] = top_key(-INFINITY, tid);                 // rows with NaN: any token
+        __syncthreads();
+    }
+    if (tid < 64) write_row(a, row, s, logit, t >= 0, chosen, lane);
 }
 
 // ---- gradient ------------------------------------------------------------------------
@@ -440,7 +509,7 @@ int logprobs_plan(const lithos_op_t& op, OpPlan* plan)
         if (splits > LITHOS_LOGPROBS_MAX_SPLITS) return fail(LITHOS_EINVAL, "logprobs: splits %lld above %d", (long long)splits, LITHOS_LOGPROBS_MAX_SPLITS);
         const bool merge = op.kind == LITHOS_OP_LOGPROBS_MERGE;
         if ((merge || splits > 1) && (!op.in[2] || !aligned16(op.in[2]))) return fail(LITHOS_EINVAL, "logprobs: a split launch and its merge need a 16-byte aligned workspace in in[2]");
-        blocks = merge ? (uint64_t)(rows + 3) / 4 : (uint64_t)rows * splits;
+        blocks = merge ? (uint64_t)rows : (uint64_t)rows * splits;
     }
     if (blocks > 0x7fffffffull) return fail(LITHOS_EINVAL, "logprobs: too many workgroups");
     plan->grid = {(uint32_t)blocks, 1, 1};
