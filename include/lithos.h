@@ -137,7 +137,7 @@ enum {
  *             codes: bytes [ceil(rows/16)][ceil(K/128)][4][16][16]: of 16 weight rows (fourth index) and 128 k, byte 4t + j of
  *             piece p (third index) holds k = 32t + 8p + j in its low and k = 32t + 8p + j + 4 in its high half (t, j = 0..3);
  *             codes beyond the matrix may hold anything.  scales, zeros: bf16 [ceil(rows/16)][ceil(K/group)][16], 16-byte
- *             aligned like the codes; zeros NULL = 8.  More than 32 rows are computed 32 at a time, the weights read for each.
+ *             aligned like the codes; zeros NULL = 8.  More than 16 rows (bf16: 32) are computed 16 (32) at a time, the weights read for each.
  * KV8_APPEND  batch,tokens,n_kv,d,pos,cap,block  k,v,[positions(i32)],scales / kcodes,vcodes   ld0=row stride of k and v
  *             k, v: rows b*tokens + t (bf16, or fp32 with IN_F32), head h at columns h*d; d = 64 or 128.  Token t of sequence b
  *             becomes position p_b + t of the cache, p_b = positions[b] or pos; a sequence with a negative position takes no
