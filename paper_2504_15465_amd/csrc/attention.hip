@@ -363,42 +363,55 @@ __global__ __launch_bounds__(256, 3) void attn_dec_kernel(AttnArgs a, AtomArgs a
 // Merge of the splits' partial softmaxes, in split order (ATTN_DEC's and ATTN_DEC8's, whose
 // workspaces are alike).  One workgroup per (sequence, key/value head).
 template <int D, bool O32>
-__global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a, AtomArgs atom)
+__global__ __launch_bounds__(1024) void attn_merge_kernel(AttnArgs a, AtomArgs atom)
 {
     const uint32_t bg = atom_logical_block(atom);
     const int b = bg / a.n_kv, g = bg % a.n_kv, S = a.splits, G = a.n_q / a.n_kv;
     const float* ws = a.ws;
     const float* ml = ws + (int64_t)a.batch * a.n_kv * S * G * D;
-    for (int i = threadIdx.x; i < G * D; i += 256) {
+    for (int i = threadIdx.x; i < G * D; i += blockDim.x) {
         const int h = i / D, d = i % D;
-        // eight splits at a time, their loads issued together (a split index beyond S re-reads the
-        // last split and is given weight 0); the sums still run in split order
+        // eight splits at a time, their loads issued together and the next eight's before they are added (a split index
+        // beyond S re-reads the last split and is given weight 0); the sums still run in split order
         const float2* mlr = reinterpret_cast<const float2*>(ml) + (int64_t)bg * S * G + h;     // split s at mlr[s * G]
         const float* wsr = ws + ((int64_t)bg * S * G + h) * D + d;                               // split s at wsr[s * G * D]
+        float2 p8[2][8];
+        float o8[2][8];
+        auto load = [&](int s0, float2 (&p)[8], float (&o)[8]) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int64_t sc = min(s0 + u, S - 1);
+                p[u] = mlr[sc * G];
+                o[u] = wsr[sc * G * D];
+            }
+        };
+        load(0, p8[0], o8[0]);                    // the first eight on their way while the maxima are looked at
         float gm = -INFINITY;
-        for (int s0 = 0; s0 < S; s0 += 8) {
+        for (int s0 = 8; s0 < S; s0 += 8) {
             float m8[8];
 #pragma unroll
             for (int u = 0; u < 8; ++u) m8[u] = mlr[(int64_t)min(s0 + u, S - 1) * G].x;
 #pragma unroll
             for (int u = 0; u < 8; ++u) gm = fmaxf(gm, m8[u]);
         }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) gm = fmaxf(gm, p8[0][u].x);
         const float ref = gm == -INFINITY ? 0.0f : gm;                      // a sequence without keys (ATTN_DEC8)
         float num = 0.0f, den = 0.0f;
-        for (int s0 = 0; s0 < S; s0 += 8) {
-            float2 p8[8];
-            float o8[8];
+        auto add = [&](int s0, const float2 (&p)[8], const float (&o)[8]) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const int64_t sc = min(s0 + u, S - 1);
-                p8[u] = mlr[sc * G];
-                o8[u] = wsr[sc * G * D];
+                const float f = s0 + u < S ? expf(p[u].x - ref) : 0.0f;     // 0 for a split without keys
+                num += o[u] * f;
+                den += p[u].y * f;
             }
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float f = s0 + u < S ? expf(p8[u].x - ref) : 0.0f;    // 0 for a split without keys
-                num += o8[u] * f;
-                den += p8[u].y * f;
+        };
+        for (int s0 = 0; s0 < S; s0 += 16) {
+            if (s0 + 8 < S) load(s0 + 8, p8[1], o8[1]);
+            add(s0, p8[0], o8[0]);
+            if (s0 + 8 < S) {
+                if (s0 + 16 < S) load(s0 + 16, p8[0], o8[0]);
+                add(s0 + 8, p8[1], o8[1]);
             }
         }
         const float r = den == 0.0f ? 0.0f : num / den;
@@ -471,6 +484,7 @@ int attn_plan(const lithos_op_t& op, OpPlan* plan)
         if (!op.in[0] || !op.out[0]) return fail(LITHOS_EINVAL, "attn_merge: null operand");
         plan->grid = {(uint32_t)n_kv, (uint32_t)batch, 1};
         plan->total = (uint32_t)(batch * n_kv);
+        plan->threads = (uint32_t)(G * d > 512 ? 1024 : G * d > 256 ? 512 : 256);
         plan->wg_per_cu = 4;
         attn_occupancy(op, plan);
         return LITHOS_OK;
@@ -504,7 +518,7 @@ int attn_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& atom,
     a.o = op.out[0];
     a.scale = op.fparam[0];
     a.flags = op.flags;
-    const dim3 grid(LITHOS_ATOM_LAUNCH_BLOCKS(atom)), block(256);
+    const dim3 grid(LITHOS_ATOM_LAUNCH_BLOCKS(atom)), block(plan.threads);
     if (op.kind == LITHOS_OP_ATTN_ENC) {
         a.batch = (int)op.dim[0]; a.n_q = (int)op.dim[1]; a.seq = (int)op.dim[2]; a.d = (int)op.dim[3];
         LITHOS_HIP(launch_kernel(attn_kernel(op), grid, block, s, a, atom));

@@ -141,19 +141,23 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, AtomAr
 
 // ---- decode attention ---------------------------------------------------------------
 //   o_h = sum_t p_ht vs_t vc_t / sum_t p_ht,   p_ht = exp(scale ks_t (q_h . kc_t) - max_t ...)
-// with kc, vc the codes and ks, vs the scales of the position's block.  The cache is read once: bound by its bytes.
+// with kc, vc the codes and ks, vs the scales of the position's block.  The cache is read once: bound by its bytes, or for
+// short sequences by the latencies of one pass.
 //
-// A workgroup owns a range of keys of one (sequence, key/value head), its four wavefronts units of 32 keys each; the
-// up to 16 query heads of the group are the column operand of MFMA 16x16x32 (columns beyond the group compute on zeros
-// and are not stored).  The contraction index of a product may be numbered in any order that both operands share:
-//  * scores S[key][head]: a lane (r = lane % 16, g = lane / 16) loads 16-byte pieces g, g + 4, .. of key row r, and
-//    step t multiplies the 8 bytes at 64 (t / 2) + 16 g + 8 (t % 2): the codes go from memory to the operand registers;
-//  * the result leaves a lane with the scores of head r and keys 4 g + e of both 16-key halves of the unit, which is the
-//    column operand of the value product if its slot (g, i) is key 16 (i / 4) + 4 g + i % 4; the row operand is
+// A workgroup owns a range of keys of one (sequence, key/value head), its wavefronts units of 32 keys each.  The
+// contraction index of a product may be numbered in any order that both operands share:
+//  * scores S[key][column] = keys x queries on MFMA 16x16x32: a lane (r = lane % 16, g = lane / 16) loads 16-byte pieces
+//    g, g + 4, .. of key row r, and step t multiplies the 8 bytes at 64 (t / 2) + 16 g + 8 (t % 2): the codes go from
+//    memory to the operand registers;
+//  * the result leaves a lane with the scores of its column and keys 4 g + e of both 16-key halves of the unit, which is
+//    the column operand of the value product if its slot (g, i) is key 16 (i / 4) + 4 g + i % 4; the row operand is
 //    V^T[d][key], and with d = (D / 16) r + j for product j a lane's piece of a value row is D / 16 bytes.
 // So neither keys, values nor probabilities pass through LDS.  Codes become bf16 exactly.  fp32 queries are three bf16
 // planes hi + mid + lo (exact); p vs is split into as many planes as the output has use for: three (exact) for fp32,
-// two (2^-16) for bf16.  Scale factors are applied to sums and probabilities in fp32.
+// two (2^-16) for bf16.  The 16 columns hold CS heads (4, 8 or 16, the group rounded up) of 16 / CS planes, so that a
+// group of up to four heads takes one product where 16 heads take one per plane; the planes' scores are added across the
+// columns, and the accumulators at the end.  Scale factors are applied to sums and probabilities in fp32; exponents are
+// powers of two.
 struct Dec8Args {
     const void* q;
     const uint8_t* k;
@@ -164,7 +168,9 @@ struct Dec8Args {
     float* ws;
     int64_t ldq;
     float scale;
-    int batch, n_q, n_kv, keys, cap, block, nblk, splits;
+    int batch, n_q, n_kv, keys, nblk, splits;
+    int64_t seq;                // bytes of a sequence's keys
+    uint32_t blk_magic;         // ceil(2^32 / (block / 16)), 0 for 16
 };
 
 // two codes (bytes 2H, 2H + 1 of w) as bf16
@@ -181,23 +187,39 @@ __device__ __forceinline__ bf16x8 codes_frag(uint32_t a, uint32_t b)
     return __builtin_bit_cast(bf16x8, make_uint4(codes_bf16<E4M3, 0>(a), codes_bf16<E4M3, 1>(a), codes_bf16<E4M3, 0>(b), codes_bf16<E4M3, 1>(b)));
 }
 
-// eight fp32 values as P bf16 planes by truncation, largest first
-template <int P>
-__device__ __forceinline__ void split_planes(const float (&x)[8], bf16x8 (&out)[P])
+// the upper halves of eight fp32 values: bf16, truncated
+__device__ __forceinline__ bf16x8 upper_halves(const float (&r)[8])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(__float_as_uint(r[2 * e + 1]), __float_as_uint(r[2 * e]), 0x07060302u);
+    return __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+}
+
+// Plane `plane` of x as an operand: x less the planes before it, truncated.  `steps` planes come before the lowest one of
+// the lanes, `most` before the highest.  Behind the third plane of 24 bits nothing is left.
+template <int STEPS, int MOST>
+__device__ __forceinline__ bf16x8 plane_operand(const float (&x)[8], int plane)
 {
     float r[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) r[e] = x[e];
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-        uint32_t w[4];
+    for (int s = 0; s < MOST && s < 2; ++s) {
+        const uint32_t mask = s < STEPS || plane > s ? 0xffff0000u : 0u;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(__float_as_uint(r[2 * e + 1]), __float_as_uint(r[2 * e]), 0x07060302u);
-        out[p] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-        if (p + 1 < P)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) r[e] -= __uint_as_float(__float_as_uint(r[e]) & 0xffff0000u);      // exact
+        for (int e = 0; e < 8; ++e) r[e] -= __uint_as_float(__float_as_uint(r[e]) & mask);             // exact
     }
+    return upper_halves(r);
+}
+
+// the sum over the 16 / CS columns of a head, in every one of them
+template <int CS>
+__device__ __forceinline__ float slot_sum(float x)
+{
+    if constexpr (CS <= 8) x += __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x128, 0xf, 0xf, true));      // row_ror:8
+    if constexpr (CS <= 4) x += __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x124, 0xf, 0xf, true));      // row_ror:4
+    return x;
 }
 
 template <int D>
@@ -207,81 +229,115 @@ struct Dec8Unit {
     float ks[2], vs[2];
 };
 
-template <int D, bool E4M3, bool Q32, bool O32>
-__global__ __launch_bounds__(256, 2) void attn_dec8_kernel(Dec8Args a, AtomArgs atom)
+constexpr float DEC8_LOG2E = 1.44269504088896340736f, DEC8_LN2 = 0.69314718055994530942f;
+
+// W wavefronts: eight share a few long ranges, which one CU would take long to fetch; four, where blocks are many, let two
+// workgroups (heads of 64: four) overlap on a CU.
+template <int D, bool E4M3, bool Q32, bool O32, int CS, int W>
+__global__ __launch_bounds__(W * 64, 2) void attn_dec8_kernel(Dec8Args a, AtomArgs atom)
 {
-    constexpr int NS = D / 32, QP = Q32 ? 3 : 1, PP = O32 ? 3 : 2, NV = D / 16, NW = D / 64;
-    __shared__ __attribute__((aligned(16))) float part_o[4][16][D];
-    __shared__ float part_m[4][16], part_l[4][16];
+    constexpr int NS = D / 32, NV = D / 16, NW = D / 64, PPO = 16 / CS;
+    constexpr int QP = Q32 ? 3 : 1, PP = O32 ? 3 : 2, NQ = (QP + PPO - 1) / PPO, NP = (PP + PPO - 1) / PPO;
+    __shared__ __attribute__((aligned(16))) float part_o[W][CS][D];
+    __shared__ float part_m[W][CS], part_l[W][CS];
 
     const uint32_t L = atom_logical_block(atom);
     const int S = a.splits;
-    const int g = L % a.n_kv, sp = (L / a.n_kv) % S, b = L / a.n_kv / S;
+    // sequences run fastest, turned by one each time: a die's contiguous share of the blocks then holds as much of a long
+    // sequence as the others', and blocks that meet on a CU are of different ones
+    const uint32_t turn = L / a.batch;
+    const int b = (L % a.batch + turn) % a.batch, g = turn % a.n_kv, sp = turn / a.n_kv;
     const int G = a.n_q / a.n_kv;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int r16 = lane & 15, kg = lane >> 4;
+    const int r16 = lane & 15, kg = lane >> 4, head = r16 % CS, slot = r16 / CS;
 
     const int T = a.lens ? max(0, min(__builtin_amdgcn_readfirstlane(a.lens[b]), a.keys)) : a.keys;
     const int U = (T + 31) / 32;
-    const int u0 = (int)((int64_t)sp * U / S), u1 = (int)((int64_t)(sp + 1) * U / S);
-
-    // queries of the group, in the scores' contraction order
-    bf16x8 qf[NS][QP];
-#pragma unroll
-    for (int t = 0; t < NS; ++t) {
-        const int64_t at = (int64_t)b * a.ldq + (int64_t)(g * G + min(r16, G - 1)) * D + 64 * (t / 2) + 16 * kg + 8 * (t % 2);
-        if constexpr (Q32) {
-            const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(a.q) + at);
-            const uint4 u = p[0], w = p[1];
-            float x[8] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w),
-                          __uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = r16 < G ? x[e] : 0.0f;
-            split_planes<QP>(x, qf[t]);
-        } else {
-            const uint4 u = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + at);
-            qf[t][0] = __builtin_bit_cast(bf16x8, r16 < G ? u : make_uint4(0, 0, 0, 0));
-        }
-    }
+    const int u0 = (int)((uint32_t)sp * (uint32_t)U / (uint32_t)S), u1 = (int)((uint32_t)(sp + 1) * (uint32_t)U / (uint32_t)S);      // 64 * 2^25 at most
 
     const uint32_t row = (uint32_t)a.n_kv * D;                       // bytes between positions
-    const uint8_t* const kbase = a.k + ((int64_t)b * a.cap * a.n_kv + g) * D;
-    const uint8_t* const vbase = a.v + ((int64_t)b * a.cap * a.n_kv + g) * D;
-    const float* const ksc = a.scales + (int64_t)b * a.nblk * a.n_kv + g;
-    const float* const vsc = ksc + (int64_t)a.batch * a.nblk * a.n_kv;
+    const uint8_t* const kbase = a.k + (int64_t)b * a.seq + g * D;
+    const uint8_t* const vbase = a.v + (int64_t)b * a.seq + g * D;
+    typedef const __attribute__((address_space(4))) float* uniform_ptr;           // read through the scalar cache
+    const uniform_ptr ksc = (uniform_ptr)(a.scales + (int64_t)b * a.nblk * a.n_kv + g), vsc = ksc + (int64_t)a.batch * a.nblk * a.n_kv;
 
     typedef Dec8Unit<D> Unit;
-    auto load = [&](Unit& x, int u) {
-        u = min(u, U - 1);                                           // a unit beyond the range is loaded, not used
-        const int last = T - 1 - 32 * u;                             // dead keys read the last live row
-        const uint8_t* const kp = kbase + (int64_t)(32 * u) * row;
-        const uint8_t* const vp = vbase + (int64_t)(32 * u) * row;
+    const uint32_t kat = (uint32_t)r16 * row + 16 * kg, vat = (uint32_t)(4 * kg) * row + NV * r16;
+    auto load_at = [&](Unit& x, const uint8_t* kp, const uint8_t* vp, auto&& koff, auto&& voff) {
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-            const uint32_t at = (uint32_t)min(16 * hf + r16, last) * row + 16 * kg;
+        for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-            for (int c = 0; c < NW; ++c) x.k[hf][c] = *reinterpret_cast<const uint4*>(kp + at + 64 * c);
-            const int64_t bl = (int64_t)(min(32 * u + 16 * hf, T - 1) / a.block) * a.n_kv;
-            x.ks[hf] = ksc[bl];
-            x.vs[hf] = vsc[bl];
-        }
+            for (int c = 0; c < NW; ++c) x.k[hf][c] = *reinterpret_cast<const uint4*>(koff(kp, hf) + 64 * c);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t at = (uint32_t)min(16 * (i / 4) + 4 * kg + i % 4, last) * row + NV * r16;
             if constexpr (NW == 2) {
-                const uint2 w = *reinterpret_cast<const uint2*>(vp + at);
+                const uint2 w = *reinterpret_cast<const uint2*>(voff(vp, i));
                 x.v[i][0] = w.x; x.v[i][1] = w.y;
             } else {
-                x.v[i][0] = *reinterpret_cast<const uint32_t*>(vp + at);
+                x.v[i][0] = *reinterpret_cast<const uint32_t*>(voff(vp, i));
             }
         }
     };
+    auto load = [&](Unit& x, int u) {
+        u = min(u, U - 1);                                           // a unit beyond the range is loaded, not used
+        const int last = T - 1 - 32 * u;
+        const uint8_t* const kp = kbase + (int64_t)(32 * u) * row;
+        const uint8_t* const vp = vbase + (int64_t)(32 * u) * row;
+        // The two cases are kept apart (the empty assembly): joined, every unit would compute the last one's addresses.
+        if (last >= 31) {                                            // one lane offset, the rows in the scalar base
+            load_at(x, kp, vp, [&](const uint8_t* q, int hf) { return q + (int64_t)(16 * hf) * row + kat; },
+                    [&](const uint8_t* q, int i) { return q + (int64_t)(16 * (i / 4) + i % 4) * row + vat; });
+            asm volatile("; whole unit");
+        } else {                                                     // dead keys read the last live row
+            load_at(x, kp, vp, [&](const uint8_t* q, int hf) { return q + (uint32_t)min(16 * hf + r16, last) * row + 16 * kg; },
+                    [&](const uint8_t* q, int i) { return q + (uint32_t)min(16 * (i / 4) + 4 * kg + i % 4, last) * row + NV * r16; });
+            asm volatile("; last unit");
+        }
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+            const uint32_t half = 2 * u + (16 * hf <= last ? hf : 0);
+            const int64_t bl = (int64_t)(a.blk_magic ? __umulhi(half, a.blk_magic) : half) * a.n_kv;
+            x.ks[hf] = ksc[bl];
+            x.vs[hf] = vsc[bl];
+        }
+    };
+    Unit x0, x1;
+    const bool busy = u0 + wave < u1;
+    if (busy) { load(x0, u0 + wave); load(x1, u0 + wave + W); }
 
-    float m = -INFINITY, l = 0.0f;             // of head r16: m the same in its four lanes, l over this lane's keys
-    f32x4 acc[NV];                             // O^T: element e of product j is d = NV (4 kg + e) + j of head r16
+    // The queries' planes, split once for all wavefronts: column c of operand o holds plane o * PPO + c / CS of head c % CS (a
+    // single plane stands in every slot), in the scores' contraction order.
+    __shared__ __attribute__((aligned(16))) uint16_t qs[NQ][16][D + 8];
+    for (int i = tid; i < NQ * 16 * (D / 8); i += W * 64) {
+        const int c8 = i % (D / 8), col = i / (D / 8) % 16, o = i / (D / 8) / 16;
+        const int h = col % CS, plane = QP == 1 ? 0 : o * PPO + col / CS;
+        const int64_t at = (int64_t)b * a.ldq + (int64_t)(g * G + min(h, G - 1)) * D + 8 * c8;
+        const bool live = h < G && plane < QP;
+        bf16x8 f;
+        if constexpr (Q32) {
+            const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(a.q) + at);
+            const uint4 u = p[0], w = p[1];
+            const float x[8] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w),
+                                __uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
+            f = plane_operand<0, 2>(x, plane);
+        } else {
+            f = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(a.q) + at));
+        }
+        *reinterpret_cast<uint4*>(&qs[o][col][8 * c8]) = live ? __builtin_bit_cast(uint4, f) : make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+    bf16x8 qf[NS][NQ];
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int o = 0; o < NQ; ++o) qf[t][o] = *reinterpret_cast<const bf16x8*>(&qs[o][r16][64 * (t / 2) + 16 * kg + 8 * (t % 2)]);
+
+    float m = -INFINITY, l = 0.0f;             // of the lane's head, exponents of two: m the same in all its lanes, l over this lane's keys
+    f32x4 acc[NV];                             // O^T: element e of product j is d = NV (4 kg + e) + j of the lane's column
 #pragma unroll
     for (int j = 0; j < NV; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float scale2 = a.scale * DEC8_LOG2E;
 
     auto compute = [&](const Unit& x, int u) {
         float s8[8];
@@ -293,48 +349,72 @@ __global__ __launch_bounds__(256, 2) void attn_dec8_kernel(Dec8Args a, AtomArgs 
                 const uint4 w = x.k[hf][t / 2];
                 const bf16x8 kf = t % 2 ? codes_frag<E4M3>(w.z, w.w) : codes_frag<E4M3>(w.x, w.y);
 #pragma unroll
-                for (int p = QP - 1; p >= 0; --p) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][p], sc, 0, 0, 0);
+                for (int p = NQ - 1; p >= 0; --p) sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][p], sc, 0, 0, 0);
             }
-            const float f = a.scale * x.ks[hf];
+            const float f = scale2 * x.ks[hf];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s8[4 * hf + e] = 32 * u + 16 * hf + 4 * kg + e < T ? sc[e] * f : -INFINITY;
+            for (int e = 0; e < 4; ++e) s8[4 * hf + e] = (QP > 1 ? slot_sum<CS>(sc[e]) : sc[e]) * f;
+        }
+        if (32 * u + 32 > T) {
+            asm volatile("; last unit");
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s8[i] = 32 * u + 16 * (i / 4) + 4 * kg + i % 4 < T ? s8[i] : -INFINITY;
         }
         float bm = s8[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) bm = fmaxf(bm, s8[i]);
         bm = fmaxf(bm, __shfl_xor(bm, 16));
         bm = fmaxf(bm, __shfl_xor(bm, 32));
-        const float nm = fmaxf(m, bm);
-        const float ref = nm == -INFINITY ? 0.0f : nm;
-        if (__any(nm > m)) {
-            const float corr = expf(m - ref);                        // 0 while m = -inf
-            l *= corr;
+        // the reference follows the largest score once that is 2^8 times as likely: nothing is lost, and few units pay for it
+        if (__any(bm > m + 8.0f)) {
+            const float nm = fmaxf(m, bm);
+            if (u != u0 + wave) {
+                const float corr = __builtin_amdgcn_exp2f(m - nm);   // m > -inf: the wavefront's first unit has live keys
+                l *= corr;
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+                for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[j][e] *= corr;
+                    for (int e = 0; e < 4; ++e) acc[j][e] *= corr;
+            }
             m = nm;
         }
+        const float ref = m;
         float p8[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float p = expf(s8[i] - ref);                       // 0 for a dead key
-            l += p;
-            p8[i] = p * x.vs[i / 4];
+            p8[i] = __builtin_amdgcn_exp2f(s8[i] - ref);             // 0 for a dead key
+            l += p8[i];
         }
-        bf16x8 pf[PP];
-        split_planes<PP>(p8, pf);
+        bf16x8 pf[NP];
+#pragma unroll
+        for (int o = 0; o < NP; ++o) {
+            const bool wanted = PPO == 1 || o * PPO + slot < PP;
+            const float vs[2] = {wanted ? x.vs[0] : 0.0f, wanted ? x.vs[1] : 0.0f};
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = p8[i] * vs[i / 4];
+            constexpr int LAST = PP - 1;
+            pf[o] = PPO >= PP ? plane_operand<0, LAST>(y, slot) : o == 0 ? plane_operand<0, PPO - 1>(y, slot) : o == 1 ? plane_operand<PPO, LAST>(y, PPO + slot) : plane_operand<2, 2>(y, 2);
+        }
 #pragma unroll
         for (int c = 0; c < NW; ++c) {
             auto product = [&](auto bb) {
-                constexpr int B = decltype(bb)::value, j0 = 0;
+                constexpr int B = decltype(bb)::value;
                 uint32_t w[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[i] = pack_bf16(code_value<E4M3, B>(x.v[2 * i][c]), code_value<E4M3, B>(x.v[2 * i + 1][c]));
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (E4M3) {
+                        // bytes B and B + 1 (B even) of two keys side by side, two of the four converted at a time
+                        const uint32_t both = __builtin_amdgcn_perm(x.v[2 * i + 1][c], x.v[2 * i][c], B < 2 ? 0x05010400u : 0x07030602u);
+                        w[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(both, 1.0f, B % 2 != 0));
+                    } else {
+                        w[i] = pack_bf16(code_value<E4M3, B>(x.v[2 * i][c]), code_value<E4M3, B>(x.v[2 * i + 1][c]));
+                    }
+                }
                 const bf16x8 vf = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-                const int j = j0 + 4 * c + B;
+                const int j = 4 * c + B;
 #pragma unroll
-                for (int p = PP - 1; p >= 0; --p) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[p], acc[j], 0, 0, 0);
+                for (int p = NP - 1; p >= 0; --p) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[p], acc[j], 0, 0, 0);
             };
             product(std::integral_constant<int, 0>{});
             product(std::integral_constant<int, 1>{});
@@ -343,41 +423,38 @@ __global__ __launch_bounds__(256, 2) void attn_dec8_kernel(Dec8Args a, AtomArgs 
         }
     };
 
-    if (u0 + wave < u1) {
-        Unit x0, x1;
-        load(x0, u0 + wave);
-        for (int u = u0 + wave; u < u1; u += 8) {
-            load(x1, u + 4);
+    if (busy)
+        for (int u = u0 + wave; u < u1; u += 2 * W) {
             compute(x0, u);
-            if (u + 4 < u1) {
-                load(x0, u + 8);
-                compute(x1, u + 4);
+            if (u + W < u1) {
+                load(x0, u + 2 * W);
+                compute(x1, u + W);
+                load(x1, u + 3 * W);
             }
         }
-    }
 
     // the wavefronts' partial softmaxes, merged in wavefront order
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (r16 < G) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int j = 0; j < NV; j += 4)
-                *reinterpret_cast<float4*>(&part_o[wave][r16][NV * (4 * kg + e) + j]) = make_float4(acc[j][e], acc[j + 1][e], acc[j + 2][e], acc[j + 3][e]);
-        if (kg == 0) { part_m[wave][r16] = m; part_l[wave][r16] = l; }
-    }
+        for (int j = 0; j < NV; j += 4) {
+            const float4 v = make_float4(slot_sum<CS>(acc[j][e]), slot_sum<CS>(acc[j + 1][e]), slot_sum<CS>(acc[j + 2][e]), slot_sum<CS>(acc[j + 3][e]));
+            if (slot == 0) *reinterpret_cast<float4*>(&part_o[wave][head][NV * (4 * kg + e) + j]) = v;
+        }
+    if (kg == 0 && slot == 0) { part_m[wave][head] = m; part_l[wave][head] = l; }
     __syncthreads();
-    for (int i = tid; i < G * D; i += 256) {
+    for (int i = tid; i < G * D; i += W * 64) {
         const int h = i / D, d = i % D;
         float gm = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) gm = fmaxf(gm, part_m[w][h]);
+        for (int w = 0; w < W; ++w) gm = fmaxf(gm, part_m[w][h]);
         const float ref = gm == -INFINITY ? 0.0f : gm;               // no key: every partial is empty
         float num = 0.0f, den = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = expf(part_m[w][h] - ref);
+        for (int w = 0; w < W; ++w) {
+            const float f = __builtin_amdgcn_exp2f(part_m[w][h] - ref);
             num += part_o[w][h][d] * f;
             den += part_l[w][h] * f;
         }
@@ -391,7 +468,7 @@ __global__ __launch_bounds__(256, 2) void attn_dec8_kernel(Dec8Args a, AtomArgs 
             a.ws[prow * D + d] = num;
             if (d == 0) {
                 float* ml = a.ws + (int64_t)a.batch * a.n_q * S * D + prow * 2;
-                ml[0] = gm;
+                ml[0] = gm * DEC8_LN2;
                 ml[1] = den;
             }
         }
@@ -403,19 +480,29 @@ __global__ __launch_bounds__(256, 2) void attn_dec8_kernel(Dec8Args a, AtomArgs 
 typedef void (*dec8_fn)(Dec8Args, AtomArgs);
 typedef void (*append_fn)(Kv8AppendArgs, AtomArgs);
 
-template <int D>
+template <int D, int CS, int W>
 static dec8_fn dec8_pick(bool e4m3, bool q32, bool o32)
 {
-    if (e4m3) return q32 ? (o32 ? attn_dec8_kernel<D, true, true, true> : attn_dec8_kernel<D, true, true, false>)
-                         : (o32 ? attn_dec8_kernel<D, true, false, true> : attn_dec8_kernel<D, true, false, false>);
-    return q32 ? (o32 ? attn_dec8_kernel<D, false, true, true> : attn_dec8_kernel<D, false, true, false>)
-               : (o32 ? attn_dec8_kernel<D, false, false, true> : attn_dec8_kernel<D, false, false, false>);
+    if (e4m3) return q32 ? (o32 ? attn_dec8_kernel<D, true, true, true, CS, W> : attn_dec8_kernel<D, true, true, false, CS, W>)
+                         : (o32 ? attn_dec8_kernel<D, true, false, true, CS, W> : attn_dec8_kernel<D, true, false, false, CS, W>);
+    return q32 ? (o32 ? attn_dec8_kernel<D, false, true, true, CS, W> : attn_dec8_kernel<D, false, true, false, CS, W>)
+               : (o32 ? attn_dec8_kernel<D, false, false, true, CS, W> : attn_dec8_kernel<D, false, false, false, CS, W>);
 }
+
+template <int D, int W>
+static dec8_fn dec8_group(const lithos_op_t& op)
+{
+    const bool e = op.flags & LITHOS_F_E4M3, q = op.flags & LITHOS_F_IN_F32, o = op.flags & LITHOS_F_OUT_F32;
+    const int64_t G = op.dim[1] / op.dim[2];
+    return G <= 4 ? dec8_pick<D, 4, W>(e, q, o) : G <= 8 ? dec8_pick<D, 8, W>(e, q, o) : dec8_pick<D, 16, W>(e, q, o);
+}
+
+static int dec8_waves(const lithos_op_t& op) { return op.dim[0] * op.dim[2] * std::max<int64_t>(1, op.dim[6]) > 256 ? 4 : 8; }
 
 static dec8_fn dec8_kernel(const lithos_op_t& op)
 {
-    const bool e = op.flags & LITHOS_F_E4M3, q = op.flags & LITHOS_F_IN_F32, o = op.flags & LITHOS_F_OUT_F32;
-    return op.dim[3] == 64 ? dec8_pick<64>(e, q, o) : dec8_pick<128>(e, q, o);
+    if (dec8_waves(op) == 4) return op.dim[3] == 64 ? dec8_group<64, 4>(op) : dec8_group<128, 4>(op);
+    return op.dim[3] == 64 ? dec8_group<64, 8>(op) : dec8_group<128, 8>(op);
 }
 
 static append_fn append_kernel(const lithos_op_t& op)
@@ -488,7 +575,8 @@ int kv8_plan(const lithos_op_t& op, OpPlan* plan)
     if (batch * n_kv * splits > 0x7fffffff) return fail(LITHOS_EINVAL, "attn_dec8: too many workgroups");
     plan->grid = {(uint32_t)(n_kv * splits), (uint32_t)batch, 1};
     plan->total = (uint32_t)(batch * n_kv * splits);
-    plan->wg_per_cu = cached_occupancy((const void*)dec8_kernel(op), 256, 2);
+    plan->threads = dec8_waves(op) * 64;
+    plan->wg_per_cu = cached_occupancy((const void*)dec8_kernel(op), (int)plan->threads, 1);
     return LITHOS_OK;
 }
 
@@ -516,18 +604,26 @@ int kv8_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& atom, 
     a.o = op.out[0];
     a.ldq = op.ld[0]; a.scale = op.fparam[0];
     a.batch = (int)op.dim[0]; a.n_q = (int)op.dim[1]; a.n_kv = (int)op.dim[2];
-    a.keys = (int)op.dim[4]; a.cap = (int)op.dim[5]; a.splits = op.dim[6] > 0 ? (int)op.dim[6] : 1; a.block = (int)op.dim[7];
-    a.nblk = (int)ceil_div(a.cap, a.block);
+    a.keys = (int)op.dim[4]; a.splits = op.dim[6] > 0 ? (int)op.dim[6] : 1;
+    a.nblk = (int)ceil_div(op.dim[5], op.dim[7]);
+    a.seq = op.dim[5] * op.dim[2] * op.dim[3];
+    // floor(h / d) = floor(h ceil(2^32 / d) / 2^32) for h < 2^26, d <= 64: the rounding adds less than h d / 2^32 / d <= 1 / d
+    a.blk_magic = op.dim[7] == 16 ? 0u : (uint32_t)ceil_div(1ll << 32, op.dim[7] / 16);
     LITHOS_HIP(launch_kernel(dec8_kernel(op), grid, block, s, a, atom));
     return LITHOS_OK;
 }
 
-// Key ranges per (sequence, key/value head): two workgroups per CU of the target, of at least four units of 32 keys each
-// (one per wavefront), so that a short sequence is not cut only to be joined again.
+// Key ranges per (sequence, key/value head).  One CU fetches some 27 bytes a nanosecond, and a launch with its merge costs
+// about 4 us: up to 128 KB a workgroup stays alone (1 sequence of 8 heads, 512 keys 9 us whole).  Beyond, ranges of at least
+// a unit for each wavefront, as many as the chip holds at a time: two workgroups of four wavefronts on a CU (heads of 64:
+// four), or, where that would be more than eight ranges to merge, one of eight.
 int kv8_split_hint(const lithos_op_t& op, int n_cus)
 {
-    const int64_t quads = ceil_div(op.dim[4], 128), want = ceil_div(2ll * n_cus, op.dim[0] * op.dim[2]);
-    return (int)std::max<int64_t>(1, std::min({quads, want, (int64_t)LITHOS_ATTN_MAX_SPLITS}));
+    const int64_t bytes = 2 * op.dim[3] * op.dim[4], pairs = op.dim[0] * op.dim[2], per_cu = op.dim[3] == 64 ? 4 : 2;
+    if (bytes <= 128 * 1024) return 1;
+    int64_t s = per_cu * n_cus / pairs;
+    if (s > 8) s = std::max<int64_t>(8, per_cu / 2 * n_cus / pairs);
+    return (int)std::max<int64_t>(1, std::min({s, ceil_div(op.dim[4], 256), (int64_t)LITHOS_ATTN_MAX_SPLITS}));
 }
 
 } // namespace lithos
