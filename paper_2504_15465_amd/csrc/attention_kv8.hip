@@ -18,13 +18,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // ---- append -----------------------------------------------------------------------
-// One wavefront per (sequence, block of positions that the new tokens touch, head, keys or values).
+// One wavefront, or of more than 16 tokens one workgroup, per (sequence, block of positions that the new tokens touch, head,
+// keys or values).
 //   s_new = max |x| / Q         (Q = 127 for int8, 448 for e4m3; the quotient rounded to fp32)
 // A block that starts with the new tokens takes s_new.  One that holds earlier positions keeps its scale s_old if
 // that is at least s_new; otherwise its earlier codes c become round(fl(fl(c s_old) / s_new)).  New codes are
 // round(fl(x / s)), 0 where s is 0 or no number.  Every step is an IEEE fp32 operation, so the result is defined to the bit.
-// Bound by the bytes of the new rows (read twice, the second time from the cache) and codes.  A lane owns eight
-// neighbouring elements of a row: 16-byte loads (two of them for fp32), 8-byte stores.
+// Bound by the bytes of the new rows and codes; 64 rows of fp32 or 128 of bf16 stay in registers between the maximum
+// and the codes, longer blocks are read twice.  A lane owns eight neighbouring elements of a row: 16-byte loads (two of them
+// for fp32), 8-byte stores.
 struct Kv8AppendArgs {
     const void* x[2];           // new keys, new values: row (b * T + t), head h at column h * d
     uint8_t* codes[2];
@@ -34,21 +36,43 @@ struct Kv8AppendArgs {
     int batch, T, n_kv, cap, block, nblk, touched;
 };
 
-__device__ __forceinline__ uint32_t quantise4(const float (&x)[8], int at, float s, bool e4m3)
+// four quotients as codes
+template <bool E4M3>
+__device__ __forceinline__ uint32_t encode4(const float (&y)[8], int at)
 {
-    float y[4];
+    if constexpr (E4M3) {
+        float c[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = s > 0.0f && s < INFINITY ? x[at + e] / s : 0.0f;      // 0 times infinity reads as NaN
-    if (e4m3) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = fminf(fmaxf(y[e], -448.0f), 448.0f);       // beyond 464 the conversion gives NaN
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+        for (int e = 0; e < 4; ++e) c[e] = __builtin_amdgcn_fmed3f(y[at + e], -448.0f, 448.0f);       // beyond 464 the conversion gives NaN
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], 0, false);
+        return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], w, true);
     }
     uint32_t w = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w |= (uint32_t)((int)fminf(fmaxf(rintf(y[e]), -127.0f), 127.0f) & 0xff) << (8 * e);
+    for (int e = 0; e < 4; ++e) w |= (uint32_t)((int)__builtin_amdgcn_fmed3f(rintf(y[at + e]), -127.0f, 127.0f) & 0xff) << (8 * e);
     return w;
+}
+
+// codes of eight elements.  The quotient by a scale of ordinary size takes two corrections with its rounded reciprocal: the
+// first leaves it within one unit of the last place, the second, whose remainder is exact, rounds it correctly (P. Markstein,
+// 1990), in five instructions where the division takes eleven.  Elements so small that a remainder would not be exact have
+// code 0 either way.
+template <bool E4M3>
+__device__ __forceinline__ uint2 quantise8(const float (&x)[8], float s, float rcp)
+{
+    float y[8];
+    if (s >= 0x1p-60f && s <= 0x1p60f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            y[e] = x[e] * rcp;
+            y[e] = fmaf(fmaf(-s, y[e], x[e]), rcp, y[e]);
+            y[e] = fmaf(fmaf(-s, y[e], x[e]), rcp, y[e]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = s > 0.0f && s < INFINITY ? x[e] / s : 0.0f;                  // 0 times infinity reads as NaN
+    }
+    return make_uint2(encode4<E4M3>(y, 0), encode4<E4M3>(y, 4));
 }
 
 // byte e of w as the number that the code stands for
@@ -66,76 +90,95 @@ __device__ __forceinline__ void code_values8(const uint2& w, float (&f)[8])
     f[4] = code_value<E4M3, 0>(w.y); f[5] = code_value<E4M3, 1>(w.y); f[6] = code_value<E4M3, 2>(w.y); f[7] = code_value<E4M3, 3>(w.y);
 }
 
-template <int D, bool X32, bool E4M3>
+template <int D, bool X32, bool E4M3, int WPU>
 __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, AtomArgs atom)
 {
-    constexpr int LPR = D / 8, RPS = 64 / LPR;          // lanes per row, rows per step
+    constexpr int LPR = D / 8, RPS = 64 / LPR * WPU, STEPS = WPU == 1 ? 1 : X32 ? 4 : 8;      // lanes per row, rows per step, steps in registers
+    __shared__ uint32_t tops[4];
     const uint32_t L = atom_logical_block(atom);
-    const int64_t unit = (int64_t)L * 4 + (threadIdx.x >> 6);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t unit = WPU == 4 ? (int64_t)L : (int64_t)L * 4 + wave;
     const int64_t units = 2ll * a.batch * a.touched * a.n_kv;
-    if (unit >= units) return;
-    const int lane = threadIdx.x & 63, c = (lane % LPR) * 8, r0 = lane / LPR;
+    if (unit >= units) return;                           // of a unit per wavefront; there are no barriers then
+    const int c = (lane % LPR) * 8, r0 = lane / LPR + (WPU == 4 ? wave * (64 / LPR) : 0);
     const int kv = unit & 1;
     const int h = (int)((unit >> 1) % a.n_kv), tb = (int)((unit >> 1) / a.n_kv % a.touched), b = (int)((unit >> 1) / a.n_kv / a.touched);
     const int64_t p0 = a.positions ? (int64_t)a.positions[b] : a.pos;
     if (p0 < 0) return;                                  // a sequence that takes no part
-    const int64_t blk = p0 / a.block + tb;
-    const int64_t first = blk * a.block;
+    const int64_t first = (p0 / a.block + tb) * a.block;
     const int64_t lo = max(p0, first), hi = min(min(p0 + a.T, first + a.block), (int64_t)a.cap);
     if (lo >= hi) return;
+    const int n = (int)(hi - lo), held = (int)(lo - first);      // new positions, earlier ones
 
-    const int64_t esz = X32 ? 4 : 2;
-    const char* src = reinterpret_cast<const char*>(a.x[kv]) + (((int64_t)b * a.T - p0) * a.ld + (int64_t)h * D + c) * esz;   // + position * ld
-    auto load = [&](int64_t p, float (&x)[8]) {
-        const uint4* at = reinterpret_cast<const uint4*>(src + p * a.ld * esz);
-        const uint4 u = at[0];
+    constexpr int64_t esz = X32 ? 4 : 2;
+    const char* const src = reinterpret_cast<const char*>(a.x[kv]) + (((int64_t)b * a.T + (lo - p0)) * a.ld + (int64_t)h * D + c) * esz;
+    struct Raw { uint4 u[X32 ? 2 : 1]; } raw[STEPS];
+    auto load = [&](int base) {                          // rows beyond the last repeat it
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const uint4* at = reinterpret_cast<const uint4*>(src + (int64_t)min(base + i * RPS + r0, n - 1) * a.ld * esz);
+#pragma unroll
+            for (int e = 0; e < (X32 ? 2 : 1); ++e) raw[i].u[e] = at[e];
+        }
+    };
+    auto unpack = [&](const Raw& r, float (&x)[8]) {
         if constexpr (X32) {
-            const uint4 v = at[1];
-            const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+            const uint32_t w[8] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w, r.u[X32].x, r.u[X32].y, r.u[X32].z, r.u[X32].w};
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(w[e]);
         } else {
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+            const uint32_t w[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(w[e] << 16); x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
         }
     };
 
+    float* const sp = a.scales + (((int64_t)kv * a.batch + b) * a.nblk + first / a.block) * a.n_kv + h;
+    const float old = held ? *sp : 0.0f;
     // largest magnitude as a bit pattern: a NaN counts as larger than everything and makes the scale NaN
     uint32_t top = 0;
-    for (int64_t p = lo + r0; p < hi; p += RPS) {
-        float x[8];
-        load(p, x);
+    for (int base = (n - 1) / (STEPS * RPS) * (STEPS * RPS); base >= 0; base -= STEPS * RPS) {
+        load(base);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+        for (int i = 0; i < STEPS; ++i) {
+            float x[8];
+            unpack(raw[i], x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+        }
     }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    const float fresh = __uint_as_float(top) / (E4M3 ? 448.0f : 127.0f);
-
-    float* const sp = a.scales + (((int64_t)kv * a.batch + b) * a.nblk + blk) * a.n_kv + h;
-    uint8_t* const dst = a.codes[kv] + ((int64_t)b * a.cap * a.n_kv + h) * D + c;
-    const int64_t row = (int64_t)a.n_kv * D;
-    float s = fresh;
-    if (lo > first) {
-        const float old = *sp;
-        const bool grown = !(fresh <= old) && old == old;       // a NaN scale stays
-        s = grown ? fresh : old;
-        if (grown)
-            for (int64_t p = first + r0; p < lo; p += RPS) {
-                uint2* at = reinterpret_cast<uint2*>(dst + p * row);
-                float x[8];
-                code_values8<E4M3>(*at, x);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] *= old;
-                *at = make_uint2(quantise4(x, 0, s, E4M3), quantise4(x, 4, s, E4M3));
-            }
+    if constexpr (WPU == 4) {
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
+        top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
     }
-    if (lane == 0) *sp = s;
-    for (int64_t p = lo + r0; p < hi; p += RPS) {
-        float x[8];
-        load(p, x);
-        *reinterpret_cast<uint2*>(dst + p * row) = make_uint2(quantise4(x, 0, s, E4M3), quantise4(x, 4, s, E4M3));
+    const float fresh = __uint_as_float(top) / (E4M3 ? 448.0f : 127.0f);
+    const bool grown = held && !(fresh <= old) && old == old;    // a NaN scale stays
+    const float s = held && !grown ? old : fresh, rcp = 1.0f / s;
+
+    const int64_t row = (int64_t)a.n_kv * D;
+    uint8_t* const dst = a.codes[kv] + (((int64_t)b * a.cap + first) * a.n_kv + h) * D + c;
+    if (grown)
+        for (int p = r0; p < held; p += RPS) {
+            uint2* at = reinterpret_cast<uint2*>(dst + p * row);
+            float x[8];
+            code_values8<E4M3>(*at, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= old;
+            *at = quantise8<E4M3>(x, s, rcp);
+        }
+    if (lane == 0 && (WPU == 1 || wave == 0) && (!held || grown)) *sp = s;
+    for (int base = 0; base < n; base += STEPS * RPS) {
+        if (base) load(base);
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) {
+            const int p = base + i * RPS + r0;
+            float x[8];
+            unpack(raw[i], x);
+            if (p < n) *reinterpret_cast<uint2*>(dst + (held + p) * row) = quantise8<E4M3>(x, s, rcp);
+        }
     }
 }
 
@@ -505,13 +548,21 @@ static dec8_fn dec8_kernel(const lithos_op_t& op)
     return op.dim[3] == 64 ? dec8_group<64, 8>(op) : dec8_group<128, 8>(op);
 }
 
+// A workgroup per block for more than 16 tokens: 8192 bf16 tokens of 8 heads of 128 took 23.9 us with a wavefront per block.
+static int append_waves(const lithos_op_t& op) { return op.dim[1] > 16 ? 4 : 1; }
+
+template <int D, int WPU>
+static append_fn append_pick(bool x32, bool e4m3)
+{
+    return x32 ? (e4m3 ? kv8_append_kernel<D, true, true, WPU> : kv8_append_kernel<D, true, false, WPU>)
+               : (e4m3 ? kv8_append_kernel<D, false, true, WPU> : kv8_append_kernel<D, false, false, WPU>);
+}
+
 static append_fn append_kernel(const lithos_op_t& op)
 {
     const bool e = op.flags & LITHOS_F_E4M3, x = op.flags & LITHOS_F_IN_F32;
-    if (op.dim[3] == 64) return x ? (e ? kv8_append_kernel<64, true, true> : kv8_append_kernel<64, true, false>)
-                                  : (e ? kv8_append_kernel<64, false, true> : kv8_append_kernel<64, false, false>);
-    return x ? (e ? kv8_append_kernel<128, true, true> : kv8_append_kernel<128, true, false>)
-             : (e ? kv8_append_kernel<128, false, true> : kv8_append_kernel<128, false, false>);
+    if (append_waves(op) == 4) return op.dim[3] == 64 ? append_pick<64, 4>(x, e) : append_pick<128, 4>(x, e);
+    return op.dim[3] == 64 ? append_pick<64, 1>(x, e) : append_pick<128, 1>(x, e);
 }
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -551,8 +602,9 @@ int kv8_plan(const lithos_op_t& op, OpPlan* plan)
         if (!aligned_to(op.in[2], 4) || !aligned_to(op.in[3], 4)) return fail(LITHOS_EINVAL, "kv8_append: misaligned positions or scales");
         if (op.ld[0] < n_kv * d || op.ld[0] % (x32 ? 4 : 8)) return fail(LITHOS_EINVAL, "kv8_append: row stride %lld is smaller than n_kv*d or breaks the 16-byte alignment of rows", (long long)op.ld[0]);
         const int64_t units = 2 * batch * touched_blocks(op) * n_kv;
-        if ((units + 3) / 4 > 0x7fffffff) return fail(LITHOS_EINVAL, "kv8_append: too many workgroups");
-        plan->grid = {(uint32_t)((units + 3) / 4), 1, 1};
+        const int64_t groups = append_waves(op) == 4 ? units : (units + 3) / 4;
+        if (groups > 0x7fffffff) return fail(LITHOS_EINVAL, "kv8_append: too many workgroups");
+        plan->grid = {(uint32_t)groups, 1, 1};
         plan->total = plan->grid.x;
         plan->wg_per_cu = cached_occupancy((const void*)append_kernel(op), 256, 4);
         return LITHOS_OK;

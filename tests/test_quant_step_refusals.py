@@ -40,7 +40,7 @@ def grad(rows=3, vocab=1000, scale=1.0, ld=None, inp=(A16[0], A16[1], A16[2], A1
 
 
 @pytest.mark.parametrize("op,blocks", [
-    (append(), 2), (append(t=40, pos=20), 4), (dec8(), 4), (dec8(splits=3), 12), (dec8(n_q=32), 4),
+    (append(), 2), (append(t=40, pos=20), 16), (dec8(), 4), (dec8(splits=3), 12), (dec8(n_q=32), 4),
     (lp(), 3), (lp(splits=4), 12), (lp(B.OP_LOGPROBS_MERGE, splits=4), 3), (lp(top=0, out=(A16[0], None), ld=(1000, 3, 0)), 3), (grad(vocab=2049), 6)])
 def test_plans(op, blocks):
     rc, p = plan(op)
