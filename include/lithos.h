@@ -164,7 +164,8 @@ enum {
  *             LOGPROBS's.  NULL gradients are zeros; rows without a given token take none from g_logprob.  May be in place.    ld2=of dlogits
  * RMSNORM     rows,H                             x,w(f32) / y                         fparam0=eps
  * ROPE_KV     rows,n_q,n_kv,d,pos,cap            qkv[rows,(n_q+2n_kv)d] (in place) / kcache,vcache   fparam0=theta
- *             qkv is bf16, or fp32 with IN_F32; the caches are always bf16 (rounded on append)
+ *             qkv is bf16, or fp32 with IN_F32; the caches are always bf16 (rounded on append); both NULL = rotate q and k only
+ *             (KV8_APPEND then appends)
  * SILU_MUL    rows,F                             gu[rows,2F] / y[rows,F]
  * IN_F32 / OUT_F32 select fp32 for in[0] / out[0] of the row kernels and of ATTN_DEC's q / o;
  * GEMM takes IN_F32 (fp32 A) only in its M <= 32 weight-streaming form.

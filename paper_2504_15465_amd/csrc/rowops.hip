@@ -512,7 +512,7 @@ __global__ __launch_bounds__(256) void rope_kv_kernel(RowArgs a, AtomArgs atom)
     const int64_t half = d / 2;
     if (slot < n_q + n_kv) {
         uint16_t* dst = nullptr;
-        if (slot >= n_q) dst = kc + ((row * cap + pos) * n_kv + (slot - n_q)) * d;
+        if (slot >= n_q && kc) dst = kc + ((row * cap + pos) * n_kv + (slot - n_q)) * d;
         for (int64_t e = lane; e < half; e += 64) {
             float inv = powf(a.f0, -2.0f * (float)e / (float)d);
             float sn, cs;
@@ -524,6 +524,7 @@ __global__ __launch_bounds__(256) void rope_kv_kernel(RowArgs a, AtomArgs atom)
             if (dst) { dst[e] = f32_to_bf16(r0); dst[e + half] = f32_to_bf16(r1); }
         }
     } else {
+        if (!vc) return;                                     // rotation only
         uint16_t* dst = vc + ((row * cap + pos) * n_kv + (slot - n_q - n_kv)) * d;
         for (int64_t e = lane; e < d; e += 64) dst[e] = f32_to_bf16(load_elem<F32>(head, hoff + e));
     }
@@ -677,7 +678,7 @@ int rowops_plan(const lithos_op_t& op, OpPlan* plan)
         const int64_t n_q = op.dim[1], n_kv = op.dim[2], d = op.dim[3], pos = op.dim[4], cap = op.dim[5];
         if (n_q <= 0 || n_kv <= 0 || d <= 0 || (d & 1) || pos < 0 || pos >= cap)
             return fail(LITHOS_EINVAL, "rope_kv: need n_q,n_kv,d > 0, d even, 0 <= pos < cap");
-        if (!op.out[0] || !op.out[1]) return fail(LITHOS_EINVAL, "rope_kv: null cache pointer");
+        if (!op.out[0] != !op.out[1]) return fail(LITHOS_EINVAL, "rope_kv: one cache pointer is null");
         blocks = ((uint64_t)rows * (n_q + 2 * n_kv) + 3) / 4;
         break;
     }

@@ -17,7 +17,9 @@ Edge dtypes (what is stored between two kernels):
                    round the other way.
 * decoder layer    every edge fp32 (weight-streaming GEMMs), except the
                    key/value cache, which is bf16: the current token's rotated
-                   key and its value are rounded when appended.
+                   key and its value are rounded when appended.  With
+                   ``q4_group`` the weights are 4-bit codes, with ``kv8_block``
+                   the cache is 8-bit codes, both with group-wise scales.
 """
 from __future__ import annotations
 
@@ -28,6 +30,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from . import quant
 from .inputs import bits_to_torch
 
 
@@ -190,39 +193,65 @@ class EncoderChain:
         self.x.copy_(torch.from_numpy(np.ascontiguousarray(x32, dtype=np.float32)))
 
 
+class _Q4Weight:
+    """A [rows, K] weight matrix in 4 bits, laid out for GEMM_Q4."""
+
+    def __init__(self, w: torch.Tensor, group: int):
+        codes, scales, zeros = quant.quantize_q4(w, group)
+        self.group = group
+        self.codes, self.scales, self.zeros = quant.pack_q4(codes), quant.pack_q4_groups(scales), quant.pack_q4_groups(zeros)
+
+
+def _product(a, w, c, m, n, k, **kw) -> B.Op:
+    """The weight-streaming product with a [n, k] matrix, bf16 or 4 bits."""
+    if isinstance(w, _Q4Weight):
+        return B.gemm_q4_op(a, w.codes, w.scales, c, m, n, k, w.group, zeros=w.zeros, **kw)
+    return B.gemm_op(a, w, c, m, n, k, tb=True, **kw)
+
+
 class DecoderChain:
-    """One decode step of a pre-norm grouped-query decoder stack against a bf16
+    """One decode step of a pre-norm grouped-query decoder stack against a
     key/value cache.  All GEMMs are the weight-streaming kind (weights [N,K],
     fp32 activations); the cache slot ``pos`` is rewritten on every step.  With
     ``fused`` (the default for at most 16 sequences) the two RMSNorms run inside
     the GEMMs that consume them and SiLU(gate) * up inside the gate/up GEMM: 7
-    launches per layer instead of 10."""
+    launches per layer instead of 10.
+
+    ``q4_group`` (32, 64 or 128) quantises the weights to 4 bits in groups of as many k: the RMSNorms are then
+    launches of their own.  ``kv8_block`` (a multiple of 16) keeps the cache in 8 bits (int8, or e4m3 with
+    ``kv8_e4m3``) with a scale per block of as many positions and head; the given prompt is quantised into it here.
+    ``head``: ``dict(rms=[H], w=[H, V] weight bits)`` makes the step end in the answer: logits, and in ``stats``
+    (log probability of ``tokens``, entropy, log-sum-exp, ``top`` log probabilities) and ``ids`` what LOGPROBS says of them."""
 
     def __init__(self, layers, kcache_bits, vcache_bits, batch: int, n_q: int, n_kv: int, pos: int, device="cuda",
-                 splits: int = 0, fused: bool = None):
+                 splits: int = 0, fused: bool = None, ctx=None, q4_group: int = 0, kv8_block: int = 0, kv8_e4m3: bool = False,
+                 head=None, top: int = 0):
         self.batch, self.n_q, self.n_kv, self.pos = batch, n_q, n_kv, pos
-        self.fused = batch <= 16 if fused is None else bool(fused)
+        self.q4_group, self.kv8_block = q4_group, kv8_block
+        if q4_group and fused:
+            raise ValueError("the fused decoder step is built on the weight-streaming GEMM with bf16 weights")
+        self.fused = (batch <= 16 and not q4_group) if fused is None else bool(fused)
         if self.fused and batch > 16:
             raise ValueError("the fused decoder step is built on the weight-streaming GEMM (at most 16 rows)")
-        # key ranges per (sequence, key/value head): enough workgroups for a few hundred CU slots
-        units = (pos + 1 + 31) // 32
-        self.splits = splits if splits > 0 else max(1, min(B.ATTN_MAX_SPLITS, units, -(-256 // (batch * n_kv))))
         H = layers[0]["w_qkv"].shape[0]
         self.H = H
         self.d = H // n_q
         self.F = layers[0]["w_d"].shape[0]
         self.cap = pos + 1
+        weight = (lambda bits: _Q4Weight(_wt(bits, device), q4_group)) if q4_group else (lambda bits: _wt(bits, device))
         self.w = []
         for L in layers:
             self.w.append(dict(rms1=_f32(L["rms1"], device), rms2=_f32(L["rms2"], device),
-                               w_qkv=_wt(L["w_qkv"], device), w_o=_wt(L["w_o"], device),
-                               w_gu=_wt(L["w_gu"], device), w_d=_wt(L["w_d"], device)))
-        self.kc, self.vc = [], []
-        for kb, vb in zip(kcache_bits, vcache_bits):
-            for src, dst in ((kb, self.kc), (vb, self.vc)):
-                c = torch.zeros((batch, self.cap, n_kv, self.d), dtype=torch.bfloat16, device=device)
-                c[:, :pos].copy_(bits_to_torch(src))
-                dst.append(c)
+                               w_qkv=weight(L["w_qkv"]), w_o=weight(L["w_o"]), w_gu=weight(L["w_gu"]), w_d=weight(L["w_d"])))
+        self.kc, self.vc, self.kv_scales = [], [], []
+        if kv8_block:
+            self._quantise_cache(kcache_bits, vcache_bits, device, torch.float8_e4m3fn if kv8_e4m3 else torch.int8, ctx)
+        else:
+            for kb, vb in zip(kcache_bits, vcache_bits):
+                for src, dst in ((kb, self.kc), (vb, self.vc)):
+                    c = torch.zeros((batch, self.cap, n_kv, self.d), dtype=torch.bfloat16, device=device)
+                    c[:, :pos].copy_(bits_to_torch(src))
+                    dst.append(c)
         f32 = torch.float32
         nqkv = (n_q + 2 * n_kv) * self.d
         self.x_in = torch.zeros((batch, H), dtype=f32, device=device)
@@ -230,10 +259,60 @@ class DecoderChain:
         self.n = torch.zeros((batch, H), dtype=f32, device=device)
         self.qkv = torch.zeros((batch, nqkv), dtype=f32, device=device)
         self.att = torch.zeros((batch, n_q * self.d), dtype=f32, device=device)
+        # key ranges per (sequence, key/value head): enough workgroups for a few hundred CU slots
+        units = (pos + 1 + 31) // 32
+        if splits > 0:
+            self.splits = splits
+        elif kv8_block:
+            self.splits = B.lithos_split_hint(self._attention(0, 1, None), 256)
+        else:
+            self.splits = max(1, min(B.ATTN_MAX_SPLITS, units, -(-256 // (batch * n_kv))))
         self.ws = torch.zeros(B.attn_workspace_floats(batch, n_q, self.d, self.splits), dtype=f32, device=device)
         self.gu = torch.zeros((batch, 2 * self.F), dtype=f32, device=device)
         self.act = torch.zeros((batch, self.F), dtype=f32, device=device)
         self.out = self.x
+        self.head = None
+        if head is not None:
+            self.head = dict(rms=_f32(head["rms"], device), w=weight(head["w"]))
+            self.vocab, self.top = head["w"].shape[1], top
+            self.logits = torch.zeros((batch, self.vocab), dtype=f32, device=device)
+            self.tokens = torch.full((batch,), -1, dtype=torch.int32, device=device)
+            self.stats = torch.zeros((batch, 3 + top), dtype=f32, device=device)
+            self.ids = torch.zeros((batch, top), dtype=torch.int32, device=device) if top else None
+            self.head_splits = B.lithos_split_hint(self._logprobs(1, None), 256)
+            self.head_ws = torch.zeros(B.logprobs_workspace_floats(batch, top, self.head_splits), dtype=f32, device=device)
+
+    def _quantise_cache(self, kcache_bits, vcache_bits, device, dtype, ctx):
+        batch, n_kv, d, block = self.batch, self.n_kv, self.d, self.kv8_block
+        own = ctx is None
+        if own:
+            ctx = B.lithos_init(torch.device(device).index or 0, None)
+        try:
+            for kb, vb in zip(kcache_bits, vcache_bits):
+                kc, vc = (torch.zeros((batch, self.cap, n_kv, d), dtype=torch.int8, device=device).view(dtype) for _ in range(2))
+                scales = torch.zeros((2, batch, -(-self.cap // block), n_kv), dtype=torch.float32, device=device)
+                if self.pos:
+                    k, v = _dev(kb, device), _dev(vb, device)
+                    torch.cuda.synchronize()
+                    B.lithos_launch_atomized(ctx, B.kv8_append_op(k, v, kc, vc, scales, batch, self.pos, n_kv, d, 0, self.cap, block))
+                    B.lithos_partition_sync(ctx)
+                self.kc.append(kc)
+                self.vc.append(vc)
+                self.kv_scales.append(scales)
+        finally:
+            if own:
+                B.lithos_shutdown(ctx)
+
+    def _attention(self, li, splits, ws) -> B.Op:
+        Bn, d, n_q, n_kv = self.batch, self.d, self.n_q, self.n_kv
+        kw = dict(ldq=(n_q + 2 * n_kv) * d, splits=splits, workspace=ws)
+        if self.kv8_block:
+            return B.attn_dec8_op(self.qkv, self.kc[li], self.vc[li], self.kv_scales[li], self.att, Bn, n_q, n_kv, d, self.pos + 1,
+                                  self.cap, self.kv8_block, 1.0 / math.sqrt(d), **kw)
+        return B.attn_dec_op(self.qkv, self.kc[li], self.vc[li], self.att, Bn, n_q, n_kv, d, self.pos + 1, self.cap, 1.0 / math.sqrt(d), **kw)
+
+    def _logprobs(self, splits, ws) -> B.Op:
+        return B.logprobs_op(self.logits, self.tokens, self.stats, self.ids, self.batch, self.vocab, self.top, splits=splits, workspace=ws)
 
     def ops(self) -> List[B.Op]:
         Bn, H, F, d, n_q, n_kv = self.batch, self.H, self.F, self.d, self.n_q, self.n_kv
@@ -245,22 +324,38 @@ class DecoderChain:
                 ops.append(B.gemm_op(self.x, W["w_qkv"], self.qkv, Bn, nqkv, H, tb=True, norm_gamma=W["rms1"]))
             else:
                 ops += [B.rmsnorm_op(self.x, W["rms1"], self.n, Bn, H),
-                        B.gemm_op(self.n, W["w_qkv"], self.qkv, Bn, nqkv, H, tb=True)]
-            ops += [
-                B.rope_kv_op(self.qkv, self.kc[li], self.vc[li], Bn, n_q, n_kv, d, self.pos, self.cap),
-                B.attn_dec_op(self.qkv, self.kc[li], self.vc[li], self.att, Bn, n_q, n_kv, d, self.pos + 1, self.cap,
-                              1.0 / math.sqrt(d), ldq=nqkv, splits=S, workspace=self.ws if S > 1 else None),
-            ]
+                        _product(self.n, W["w_qkv"], self.qkv, Bn, nqkv, H)]
+            if self.kv8_block:
+                kv = self.qkv[:, n_q * d:]
+                ops += [B.rope_kv_op(self.qkv, None, None, Bn, n_q, n_kv, d, self.pos, self.cap),
+                        B.kv8_append_op(kv, kv[:, n_kv * d:], self.kc[li], self.vc[li], self.kv_scales[li], Bn, 1, n_kv, d, self.pos,
+                                        self.cap, self.kv8_block, ldx=nqkv)]
+            else:
+                ops.append(B.rope_kv_op(self.qkv, self.kc[li], self.vc[li], Bn, n_q, n_kv, d, self.pos, self.cap))
+            ops.append(self._attention(li, S, self.ws if S > 1 else None))
             if S > 1:
                 ops.append(B.attn_merge_op(self.ws, self.att, Bn, n_q, n_kv, d, S))
-            ops.append(B.gemm_op(self.att, W["w_o"], self.x, Bn, H, n_q * d, tb=True, residual=self.x))
+            ops.append(_product(self.att, W["w_o"], self.x, Bn, H, n_q * d, residual=self.x))
             if self.fused:
                 ops.append(B.gemm_op(self.x, W["w_gu"], self.act, Bn, F, H, tb=True, norm_gamma=W["rms2"], glu=True))
             else:
-                ops += [B.rmsnorm_op(self.x, W["rms2"], self.n, Bn, H),
-                        B.gemm_op(self.n, W["w_gu"], self.gu, Bn, 2 * F, H, tb=True),
-                        B.silu_mul_op(self.gu, self.act, Bn, F)]
-            ops.append(B.gemm_op(self.act, W["w_d"], self.x, Bn, H, F, tb=True, residual=self.x))
+                ops.append(B.rmsnorm_op(self.x, W["rms2"], self.n, Bn, H))
+                if self.q4_group and F % 16 == 0:
+                    ops.append(_product(self.n, W["w_gu"], self.act, Bn, F, H, glu=True))
+                else:
+                    ops += [_product(self.n, W["w_gu"], self.gu, Bn, 2 * F, H),
+                            B.silu_mul_op(self.gu, self.act, Bn, F)]
+            ops.append(_product(self.act, W["w_d"], self.x, Bn, H, F, residual=self.x))
+        if self.head is not None:
+            V, S = self.vocab, self.head_splits
+            if self.fused:
+                ops.append(B.gemm_op(self.x, self.head["w"], self.logits, Bn, V, H, tb=True, norm_gamma=self.head["rms"]))
+            else:
+                ops += [B.rmsnorm_op(self.x, self.head["rms"], self.n, Bn, H),
+                        _product(self.n, self.head["w"], self.logits, Bn, V, H)]
+            ops.append(self._logprobs(S, self.head_ws if S > 1 else None))
+            if S > 1:
+                ops.append(B.logprobs_merge_op(self.head_ws, self.logits, self.tokens, self.stats, self.ids, Bn, V, self.top, S))
         for i, o in enumerate(ops):
             o.op_id = i
         return ops
