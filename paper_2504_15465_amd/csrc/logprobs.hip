@@ -9,9 +9,9 @@
 //
 // The most likely tokens: every lane notes the largest of its elements in each of up to eight stretches.  If m of the four
 // wavefronts have j lanes each, m j >= top, whose largest element reaches a bound, so do `top` elements, all of them in the
-// few stretches whose largest does; the bound is the best for m = 4, 2 and 1.  The elements of these stretches are read a
-// second time; those that reach the bound find their places by counting larger ones.  (A list kept during the pass cost
-// more: 2048 rows of 131072 bf16 took 132 us with top = 5 and 171 with 32, against 105 without tokens.)
+// few stretches whose largest does; the bound is the best for m = 4, 2 and 1.  The elements of these stretches are read a second time (if a wavefront has a single tile, it is still in registers); those that
+// reach the bound find their places by counting larger ones.  (A list kept during the pass cost more: 2048 rows of 131072
+// bf16 took 132 us with top = 5 and 171 with 32, against 105 without tokens.)
 // Bound by the bytes of the logits, read once.
 #include "common.hpp"
 #include <math.h>
@@ -38,17 +38,17 @@ typedef uint32_t u32x4_b2 __attribute__((ext_vector_type(4), aligned(2)));
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
-// larger key = larger value, then lower index; -0 is 0
-__device__ __forceinline__ uint64_t top_key(float x, uint32_t idx)
+// larger number = larger value; -0 is 0
+__device__ __forceinline__ uint32_t ordered(float x)
 {
     const uint32_t b = __float_as_uint(x + 0.0f);
-    return ((uint64_t)(b ^ (b & 0x80000000u ? 0xffffffffu : 0x80000000u)) << 32) | (0xffffffffu - idx);
+    return b ^ (b & 0x80000000u ? 0xffffffffu : 0x80000000u);
 }
-__device__ __forceinline__ float key_value(uint64_t k)
-{
-    const uint32_t b = (uint32_t)(k >> 32);
-    return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
-}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
+
+// larger key = larger value, then lower index
+__device__ __forceinline__ uint64_t top_key(float x, uint32_t idx) { return ((uint64_t)ordered(x) << 32) | (0xffffffffu - idx); }
+__device__ __forceinline__ float key_value(uint64_t k) { return value_of((uint32_t)(k >> 32)); }
 __device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xffffffffu - (uint32_t)k; }
 
 // sums of a softmax over some elements, d in powers of two
@@ -67,38 +67,69 @@ __device__ __forceinline__ Soft soft_join(const Soft& a, const Soft& b, float c2
     return r;
 }
 
-__device__ __forceinline__ Soft soft_wave(Soft s, float c2)
+// x of the lane that the DPP control names (within a row of 16)
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true)); }
+
+template <typename Op>
+__device__ __forceinline__ float wave_all(float x, Op op)
 {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const Soft b = {__shfl_xor(s.m, o), __shfl_xor(s.l, o), __shfl_xor(s.t, o)};
-        s = soft_join(s, b, c2);
-    }
-    return s;
+    x = op(x, from_lane<0x121>(x));               // row_ror by 1, 2, 4, 8
+    x = op(x, from_lane<0x122>(x));
+    x = op(x, from_lane<0x124>(x));
+    x = op(x, from_lane<0x128>(x));
+    x = op(x, __shfl_xor(x, 16));
+    return op(x, __shfl_xor(x, 32));
 }
 
-// one lane's key, the same in every lane
-__device__ __forceinline__ uint64_t key_of_lane(uint64_t k, int lane)
+// The least of the maxima of the lanes' residue classes modulo `groups`, a power of two.
+__device__ __forceinline__ uint32_t least_of_groups(uint32_t x, int groups)
 {
-    return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
+    auto step = [&](uint32_t y, int stride) { x = stride >= groups ? max(x, y) : min(x, y); };
+    step((uint32_t)__shfl_xor((int)x, 32), 32);
+    step((uint32_t)__shfl_xor((int)x, 16), 16);
+    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true), 8);     // row_ror: modulo 16 the neighbour at that distance
+    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, true), 4);
+    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, true), 2);
+    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, true), 1);
+    return x;
+}
+
+__device__ __forceinline__ int power_of_two_from(int n) { return n <= 1 ? 1 : 1 << (32 - __clz(n - 1)); }
+
+// the sums of a wavefront's lanes, referred to the largest of their references
+__device__ __forceinline__ Soft soft_wave(const Soft& s, float c2)
+{
+    Soft r;
+    r.m = wave_all(s.m, [](float a, float b) { return fmaxf(a, b); });
+    const float d = fmaxf((s.m - (r.m == -INFINITY ? 0.0f : r.m)) * c2, -300.0f), f = __builtin_amdgcn_exp2f(d);
+    r.l = wave_all(f * s.l, [](float a, float b) { return a + b; });
+    r.t = wave_all(f * fmaf(d, s.l, s.t), [](float a, float b) { return a + b; });
+    return r;
 }
 
 // The k largest of n distinct keys in LDS, sorted, to `out`: a key's place is the number of larger ones.  By the whole
-// workgroup; the caller puts barriers around it.
+// workgroup, up to eight neighbouring threads to a key; the caller puts barriers around it.
 __device__ __forceinline__ void choose_top(const uint64_t* keys, int n, int k, uint64_t* out)
 {
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const uint64_t mine = keys[i];
-        int above = 0, o = 0;
-        for (; o + 8 <= n; o += 8) {
-            uint64_t other[8];
+    const int share = n > 128 ? 0 : n > 64 ? 1 : n > 32 ? 2 : 3;                 // log2 of the threads to a key
+    const int part = threadIdx.x & ((1 << share) - 1), stride = 4 << share;
+    for (int i0 = 0; i0 < n; i0 += 256 >> share) {
+        const int i = i0 + (threadIdx.x >> share);
+        const uint64_t mine = keys[min(i, n - 1)];
+        int above = 0;
+#pragma unroll 2
+        for (int o = 4 * part; o < n; o += stride) {
+            uint64_t other[4];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) other[u] = keys[o + u];
+            for (int u = 0; u < 4; ++u) other[u] = keys[min(o + u, n - 1)];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) above += other[u] > mine;
+            for (int u = 0; u < 4; ++u) above += o + u < n && other[u] > mine;
         }
-        for (; o < n; ++o) above += keys[o] > mine;
-        if (above < k) out[above] = mine;
+        if (share >= 1) above += __shfl_xor(above, 1);
+        if (share >= 2) above += __shfl_xor(above, 2);
+        if (share >= 3) above += __shfl_xor(above, 4);
+        if (i < n && part == 0 && above < k) out[above] = mine;
     }
 }
 
@@ -145,6 +176,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
     __shared__ uint64_t chosen[LP_TOP];
     __shared__ Soft softs[4];
     __shared__ float nth[3][4];                   // per wavefront: its ceil(K / 4)-th, ceil(K / 2)-th and K-th largest lane maximum
+    __shared__ uint4 tops[4][16];                 // the wavefronts' lane maxima, ordered
     __shared__ float peaks[LP_SEG][256];          // largest elements of the lanes' stretches
     __shared__ uint16_t sel[LP_SEG * 256];
     __shared__ int n_sel, n_cand;
@@ -233,16 +265,22 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
     }
 
     if (K) {
-        int above = 0;
-#pragma unroll 8
-        for (int o = 0; o < 64; ++o) above += __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(most), o)) > most;
+        const uint32_t mine = ordered(most);
+        reinterpret_cast<uint32_t*>(tops[wave])[lane] = mine;
+        wave_lds_sync();
+        int above = 0;                            // (through scalar registers, a lane at a time, this took 4000 cycles)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const uint4 o = tops[wave][q];
+            above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+        }
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
             // of the maxima that fewer than j lanes exceed the least one: with equal ones it is exceeded by fewer than j - 1
             int c = (K + (4 >> i) - 1) / (4 >> i) - 1;
             uint64_t at;
             while ((at = __ballot(above == c)) == 0) --c;
-            if (lane == 0) nth[i][wave] = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(most), __ffsll((unsigned long long)at) - 1));
+            if (lane == __ffsll((unsigned long long)at) - 1) nth[i][wave] = most;
         }
         if (tid == 0) n_sel = n_cand = 0;
     }
@@ -254,23 +292,14 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
         float bound = fminf(fminf(nth[0][0], nth[0][1]), fminf(nth[0][2], nth[0][3]));
         bound = fmaxf(bound, fmaxf(fminf(hi01, hi23), fmaxf(lo01, lo23)));                 // second largest
         bound = fmaxf(bound, fmaxf(fmaxf(nth[2][0], nth[2][1]), fmaxf(nth[2][2], nth[2][3])));
-        for (int g = 0; g < seg; ++g) {
-            const float p = peaks[g][tid];
-            if (p >= bound && p > -INFINITY) sel[atomicAdd(&n_sel, 1)] = (uint16_t)(g * 256 + tid);     // in any order, as below: places follow from keys
-        }
-        __syncthreads();
-        constexpr int RUNS = 16 / RUN;
-        const int ns = n_sel, items = ns * len * RUNS;
-        // elements above `floor` (a key) of item i, a run of a stretch, to the candidates
-        auto scan = [&](int i, uint64_t floor) {
-            const int who = sel[i / (RUNS * len)] & 255, g = sel[i / (RUNS * len)] >> 8, q = i % RUNS, tile = t0 + (who >> 6) + 4 * (g * len + i / RUNS % len);
-            if (tile >= t1) return;
+        // elements above `floor` (a key) of a run to the candidates
+        auto offer = [&](const u32x4& v, int tile, int l, int q, uint64_t floor) {
             float x[RUN];
-            unpack(load(tile, who & 63, q), x);
+            unpack(v, x);
 #pragma unroll
             for (int e = 0; e < RUN; ++e)
                 if (x[e] >= bound && x[e] > -INFINITY) {
-                    const uint64_t k = top_key(x[e], index(tile, who & 63, RUN * q + e));
+                    const uint64_t k = top_key(x[e], index(tile, l, RUN * q + e));
                     if (k > floor) {
                         const int at = atomicAdd(&n_cand, 1);
                         if (at < LP_ROOM + LP_TOP) cand[at] = k;
@@ -280,17 +309,66 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
         // of forbidden tokens, where fewer than K are allowed, the first K suffice
         auto fill = [&]() {
             const int i = t0 * TILE + tid;
-            if (bound == -INFINITY && tid < K && i < min(t1 * TILE, a.vocab) && logit_at<X32>(a, row, i) == -INFINITY) cand[atomicAdd(&n_cand, 1)] = top_key(-INFINITY, i);
+            if (bound == -INFINITY && tid < K && i < min(t1 * TILE, a.vocab) && logit_at<X32>(a, row, i) == -INFINITY) {
+                const int at = atomicAdd(&n_cand, 1);
+                if (at < LP_ROOM + LP_TOP) cand[at] = top_key(-INFINITY, i);
+            }
+        };
+        constexpr int RUNS = 16 / RUN;
+        const bool at_hand = turns == 1;              // a tile for each wavefront at most: it is still in registers
+        auto select = [&]() {
+            for (int g = 0; g < seg; ++g) {
+                const float p = peaks[g][tid];
+                if (p >= bound && p > -INFINITY) sel[atomicAdd(&n_sel, 1)] = (uint16_t)(g * 256 + tid);     // in any order: places follow from keys
+            }
         };
         fill();
-        for (int i = tid; i < items; i += 256) scan(i, 0);
+        if (!at_hand) {
+            select();
+        } else if (t0 + wave < t1) {
+            float x[16];
+            uint32_t mine = 0;
+#pragma unroll
+            for (int q = 0; q < RUNS; ++q) unpack(raw[q], x + RUN * q);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) mine |= (x[e] >= bound && x[e] > -INFINITY ? 1u : 0u) << e;
+            // the wavefront's places behind one another, lane by lane
+            const int n = __popc(mine);
+            int at = 0, total = 0;
+#pragma unroll
+            for (int b = 0; b < 5; ++b) {             // 16 at most
+                const uint64_t m = __ballot((n >> b) & 1);
+                at += __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0)) << b;
+                total += __popcll(m) << b;
+            }
+            int base = 0;
+            if (lane == 0) base = atomicAdd(&n_cand, total);
+            at += __builtin_amdgcn_readfirstlane(base);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (mine >> e & 1) {
+                    if (at < LP_ROOM + LP_TOP) cand[at] = top_key(x[e], index(t0 + wave, lane, e));
+                    ++at;
+                }
+        }
         __syncthreads();
+        // item i, a run of a stretch
+        auto scan = [&](int i, uint64_t floor) {
+            const int who = sel[i / (RUNS * len)] & 255, g = sel[i / (RUNS * len)] >> 8, q = i % RUNS, tile = t0 + (who >> 6) + 4 * (g * len + i / RUNS % len);
+            if (tile < t1) offer(load(tile, who & 63, q), tile, who & 63, q, floor);
+        };
+        if (!at_hand) {
+            for (int i = tid; i < n_sel * len * RUNS; i += 256) scan(i, 0);
+            __syncthreads();
+        }
         int n = n_cand;
         if (n > LP_ROOM) {
             // many equal values: 256 items at a time, and only what is above the K-th chosen so far
             __syncthreads();
+            if (at_hand) select();
             if (tid == 0) n_cand = 0;
             __syncthreads();
+            const int items = n_sel * len * RUNS;
             fill();
             n = 0;
             for (int i0 = 0; i0 < items; i0 += 256) {
@@ -305,7 +383,6 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
                 __syncthreads();
             }
         }
-        __syncthreads();
         choose_top(cand, n, K, chosen);
         __syncthreads();
         n = min(n, K);
@@ -331,8 +408,8 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
     }
 }
 
-// Joins the splits of a row: one workgroup per row.  With j = ceil(top / splits) at least `top` keys are as large as the
-// ceil(top / j)-th largest of the splits' j-th keys; the few that are find their places by counting larger ones.
+// Joins the splits of a row: one workgroup per row.  With j = ceil(top / splits) at least `top` keys reach the least of the
+// largest j-th keys of ceil(top / j) groups of splits; the few that do find their places by counting larger ones.
 template <bool X32>
 __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobArgs a, AtomArgs atom)
 {
@@ -348,21 +425,22 @@ __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobArgs a, Atom
         const uint2 k = reinterpret_cast<const uint2*>(ws + sp * stride + 4)[j];
         return ((uint64_t)k.y << 32) | k.x;
     };
+    // everything is fetched at once: the splits' sums and j-th keys, this thread's first key, the given token's logit
     Soft s = {-INFINITY, 0.0f, 0.0f};
     const int t = given_token(a, row);
     float logit = 0.0f;
+    uint64_t mine = 0;
+    if (tid < S * K) mine = key_at(tid / K, tid % K);
+    const int mine_of = tid < S * K ? (int)ws[tid / K * stride + 3] : 0;
+    const int j = K ? (K + S - 1) / S : 1, m = K ? (K + j - 1) / j : 1;
     if (tid < 64) {
-        if (t >= 0) logit = logit_at<X32>(a, row, t);
         const f32x4_b4 p = lane < S ? *reinterpret_cast<const f32x4_b4*>(ws + lane * stride) : f32x4_b4{-INFINITY, 0.0f, 0.0f, 0.0f};
+        uint64_t jth = K && lane < S ? key_at(lane, j - 1) : 0;
+        if (t >= 0) logit = logit_at<X32>(a, row, t);
         if (K) {
-            const int j = (K + S - 1) / S, m = (K + j - 1) / j;
-            const uint64_t mine = lane < S && (int)p.w >= j ? key_at(lane, j - 1) : 0;
-            int above = 0;
-#pragma unroll 8
-            for (int o = 0; o < 64; ++o) above += key_of_lane(mine, o) > mine;
-            const uint64_t at = __ballot(above == m - 1 && mine != 0);
-            if (lane == 0) { n_cand = 0; bound_s = 0; }
-            if (at && lane == __ffsll((unsigned long long)at) - 1) bound_s = mine;
+            if ((int)p.w < j) jth = 0;
+            const uint32_t v = least_of_groups((uint32_t)(jth >> 32), power_of_two_from(m));         // 0: not as many splits
+            if (lane == 0) { n_cand = 0; bound_s = (uint64_t)v << 32; }
         }
         s = soft_wave(Soft{p.x, p.y, p.z}, c2);
     }
@@ -370,16 +448,15 @@ __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobArgs a, Atom
         __syncthreads();
         const uint64_t bound = bound_s;
         for (int i = tid; i < S * K; i += 256) {
-            const int sp = i / K, j = i % K;
-            if (j < (int)ws[sp * stride + 3]) {
-                const uint64_t k = key_at(sp, j);
-                if (k >= bound) cand[atomicAdd(&n_cand, 1)] = k;        // in any order: places follow from the keys
-            }
+            const int sp = i / K, q = i % K;
+            const bool there = q < (i == tid ? mine_of : (int)ws[sp * stride + 3]);
+            const uint64_t k = !there ? 0 : i == tid ? mine : key_at(sp, q);
+            if (there && k >= bound) cand[atomicAdd(&n_cand, 1)] = k;           // in any order: places follow from the keys
         }
         __syncthreads();
         const int n = n_cand;
         choose_top(cand, n, K, chosen);
-        if (tid >= n && tid < K) chosen[tid] = top_key(-INFINITY, tid);                 // rows with NaN: any token
+        if (tid >= n && tid < K) chosen[tid] = top_key(-INFINITY, tid);         // rows with NaN: any token
         __syncthreads();
     }
     if (tid < 64) write_row(a, row, s, logit, t >= 0, chosen, lane);
