@@ -511,7 +511,8 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobGradArgs a, A
     }
 #pragma unroll
     for (int e = 0; e < RUN; ++e) {
-        const float lp = fmaf(c, x[e], -lse), p = __builtin_amdgcn_exp2f(lp * LOG2E);
+        // p is 0 well above -300; a mask of the type's lowest value must not become 0 times infinity below
+        const float lp = fmaxf(fmaf(c, x[e], -lse), -300.0f), p = __builtin_amdgcn_exp2f(lp * LOG2E);
         float dz = -p * fmaf(ge, lp + H, g);
         if (i0 + e == t) dz += g;
         if (x[e] == -INFINITY) dz = 0.0f;

@@ -286,14 +286,15 @@ class DecoderChain:
         batch, n_kv, d, block = self.batch, self.n_kv, self.d, self.kv8_block
         own = ctx is None
         if own:
-            ctx = B.lithos_init(torch.device(device).index or 0, None)
+            index = torch.device(device).index
+            ctx = B.lithos_init(torch.cuda.current_device() if index is None else index, None)
         try:
             for kb, vb in zip(kcache_bits, vcache_bits):
                 kc, vc = (torch.zeros((batch, self.cap, n_kv, d), dtype=torch.int8, device=device).view(dtype) for _ in range(2))
                 scales = torch.zeros((2, batch, -(-self.cap // block), n_kv), dtype=torch.float32, device=device)
                 if self.pos:
                     k, v = _dev(kb, device), _dev(vb, device)
-                    torch.cuda.synchronize()
+                    torch.cuda.synchronize(device)
                     B.lithos_launch_atomized(ctx, B.kv8_append_op(k, v, kc, vc, scales, batch, self.pos, n_kv, d, 0, self.cap, block))
                     B.lithos_partition_sync(ctx)
                 self.kc.append(kc)

@@ -663,3 +663,28 @@ def test_grad_of_forbidden_tokens_and_in_place(dt):
     assert bits_equal(own, dx)
 
 
+
+
+@pytest.mark.parametrize("dt", [F32, BF])
+@pytest.mark.parametrize("scale", [1.0, 2.0])
+def test_grad_of_tokens_masked_by_the_lowest_value(dt, scale):
+    rows, vocab = 4, 2500
+    x = logits(rows, vocab, dt)
+    x[torch.rand(rows, vocab, generator=rnd(54)) < 0.4] = torch.finfo(dt).min
+    x[:, 5], x[3, 6] = 1.0, torch.finfo(dt).min
+    tokens = [5, 5, -1, 6]
+    stats, _ = lp_run(x, vocab, tokens, 0, scale=scale, pad=0)
+    glp, gent = torch.tensor([0.7, 0.0, -1.3, 0.4]), torch.tensor([3.0, -2.5, 1.5, 0.0])
+    dx = grad_run(x, vocab, tokens, stats, glp, gent, scale, dt)
+    want, tol = grad_plain(x, tokens, stats.cpu(), glp, gent, scale)
+    check(dx, want, tol + (half_step(BF) * (want.abs() + tol) if dt == BF else 2 * U * want.abs()) + 1e-38)
+
+
+def test_grad_of_rows_with_what_is_no_number():
+    rows, vocab = 3, 700
+    x = logits(rows, vocab, F32)
+    x[1, 300], x[2, 7] = math.nan, math.inf
+    stats, _ = lp_run(x, vocab, [1] * rows, 0, pad=0)
+    for glp, gent in ((torch.ones(rows), None), (None, torch.ones(rows))):
+        dx = grad_run(x, vocab, [1] * rows, stats, glp, gent, 1.0, F32)
+        assert bool(torch.isfinite(dx[0]).all()) and bool(torch.isnan(dx[1:]).all())
