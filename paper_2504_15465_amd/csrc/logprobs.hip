@@ -620,11 +620,15 @@ int logprobs_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& a
     return LITHOS_OK;
 }
 
-// Two workgroups per CU of the target, each with a tile of 1024 for every one of its four wavefronts.
+// Two workgroups per CU of the target, each with a tile of 1024 for every one of its four wavefronts.  A second launch costs
+// what a workgroup takes for some 40000 tokens: rows whose other pieces have no more than that stay whole.  Whole / split, us a
+// pass: 33 x 32003 11.8 / 12.6, 150 x 50001 13.6 / 15, 400 x 50001 16.9 / 20.7, 1 x 32000 10.1 / 9.3 (bf16); 4 x 50257
+// 12.9 / 9.9, 4 x 131072 22.8 / 9.9 (fp32), 64 x 131072 22 / 13.8, 300 x 131072 28.6 / 26.9, 400 x 131072 31 / 32.1.
 int logprobs_split_hint(const lithos_op_t& op, int n_cus)
 {
-    const int64_t quads = (op.dim[1] + 4095) / 4096, want = (2ll * n_cus + op.dim[0] - 1) / op.dim[0];
-    return (int)std::max<int64_t>(1, std::min({quads, want, (int64_t)LITHOS_LOGPROBS_MAX_SPLITS}));
+    const int64_t vocab = op.dim[1], quads = (vocab + 4095) / 4096, want = (2ll * n_cus + op.dim[0] - 1) / op.dim[0];
+    const int64_t s = std::max<int64_t>(1, std::min({quads, want, (int64_t)LITHOS_LOGPROBS_MAX_SPLITS}));
+    return vocab - vocab / s > 40000 ? (int)s : 1;
 }
 
 } // namespace lithos
