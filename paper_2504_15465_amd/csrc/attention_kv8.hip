@@ -102,10 +102,12 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, AtomAr
     if (unit >= units) return;                           // of a unit per wavefront; there are no barriers then
     const int c = (lane % LPR) * 8, r0 = lane / LPR + (WPU == 4 ? wave * (64 / LPR) : 0);
     const int kv = unit & 1;
-    const int h = (int)((unit >> 1) % a.n_kv), tb = (int)((unit >> 1) / a.n_kv % a.touched), b = (int)((unit >> 1) / a.n_kv / a.touched);
+    const uint32_t pair = (uint32_t)(unit >> 1), block_of = pair / (uint32_t)a.n_kv;          // below 2^32; divisions of 64 bits are long
+    const int h = (int)(pair % (uint32_t)a.n_kv), tb = (int)(block_of % (uint32_t)a.touched), b = (int)(block_of / (uint32_t)a.touched);
     const int64_t p0 = a.positions ? (int64_t)a.positions[b] : a.pos;
     if (p0 < 0) return;                                  // a sequence that takes no part
-    const int64_t first = (p0 / a.block + tb) * a.block;
+    const uint32_t blk = (uint32_t)p0 / (uint32_t)a.block + tb;                               // p0 < 2^31
+    const int64_t first = (int64_t)blk * a.block;
     const int64_t lo = max(p0, first), hi = min(min(p0 + a.T, first + a.block), (int64_t)a.cap);
     if (lo >= hi) return;
     const int n = (int)(hi - lo), held = (int)(lo - first);      // new positions, earlier ones
@@ -133,7 +135,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, AtomAr
         }
     };
 
-    float* const sp = a.scales + (((int64_t)kv * a.batch + b) * a.nblk + first / a.block) * a.n_kv + h;
+    float* const sp = a.scales + (((int64_t)kv * a.batch + b) * a.nblk + blk) * a.n_kv + h;
     const float old = held ? *sp : 0.0f;
     // largest magnitude as a bit pattern: a NaN counts as larger than everything and makes the scale NaN
     uint32_t top = 0;
@@ -288,8 +290,10 @@ __global__ __launch_bounds__(W * 64, 2) void attn_dec8_kernel(Dec8Args a, AtomAr
     const int S = a.splits;
     // sequences run fastest, turned by one each time: a die's contiguous share of the blocks then holds as much of a long
     // sequence as the others', and blocks that meet on a CU are of different ones
-    const uint32_t turn = L / a.batch;
-    const int b = (L % a.batch + turn) % a.batch, g = turn % a.n_kv, sp = turn / a.n_kv;
+    uint32_t turn = L, b = 0, g = 0, sp = 0;                          // divisions only where there is something to divide
+    if (a.batch > 1) { turn = L / a.batch; b = (L % a.batch + turn) % a.batch; }
+    if (turn < (uint32_t)a.n_kv) g = turn;
+    else { sp = turn / a.n_kv; g = turn % a.n_kv; }
     const int G = a.n_q / a.n_kv;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -297,7 +301,7 @@ __global__ __launch_bounds__(W * 64, 2) void attn_dec8_kernel(Dec8Args a, AtomAr
 
     const int T = a.lens ? max(0, min(__builtin_amdgcn_readfirstlane(a.lens[b]), a.keys)) : a.keys;
     const int U = (T + 31) / 32;
-    const int u0 = (int)((uint32_t)sp * (uint32_t)U / (uint32_t)S), u1 = (int)((uint32_t)(sp + 1) * (uint32_t)U / (uint32_t)S);      // 64 * 2^25 at most
+    const int u0 = S == 1 ? 0 : (int)(sp * (uint32_t)U / (uint32_t)S), u1 = S == 1 ? U : (int)((sp + 1) * (uint32_t)U / (uint32_t)S);   // 64 * 2^25 at most
 
     const uint32_t row = (uint32_t)a.n_kv * D;                       // bytes between positions
     const uint8_t* const kbase = a.k + (int64_t)b * a.seq + g * D;

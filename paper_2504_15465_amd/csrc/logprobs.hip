@@ -182,12 +182,13 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
     __shared__ int n_sel, n_cand;
 
     const uint32_t L = atom_logical_block(atom);
-    const int64_t row = L / a.splits;
-    const int sp = L % a.splits;
+    const uint32_t S = a.splits;
+    const int64_t row = S == 1 ? L : L / S;
+    const uint32_t sp = S == 1 ? 0 : L % S;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tiles = (a.vocab + TILE - 1) / TILE;
-    const int t0 = (int)((int64_t)sp * tiles / a.splits), t1 = (int)((int64_t)(sp + 1) * tiles / a.splits);
+    const int t0 = S == 1 ? 0 : (int)(sp * tiles / S), t1 = S == 1 ? tiles : (int)((sp + 1) * tiles / S);        // 64 * 2^20 at most
     const float c2 = a.scale * LOG2E;
     const int K = a.top;
 
