@@ -285,7 +285,7 @@ int lithos_op_grid(lithos_ctx_t* ctx, const lithos_op_t* op, lithos_dim3* grid_o
  * (slices * M * ldc floats) and follows the GEMM with SUM_SLICES. */
 int lithos_gemm_split_hint(const lithos_op_t* op, int32_t n_cus, int32_t* tile_out, int32_t* slices_out);
 
-/* Splits that put about two workgroups on each of `n_cus` compute units for an ATTN_DEC8 or a
+/* Splits that put one or two workgroups on each of `n_cus` compute units for an ATTN_DEC8 or a
  * LOGPROBS descriptor (its own splits and workspace are not looked at); 1 = launch it whole, also
  * where a second launch would take longer than it saves.  For more than 1 the caller
  * provides the workspace and follows with ATTN_MERGE or LOGPROBS_MERGE. */

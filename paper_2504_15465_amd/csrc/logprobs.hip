@@ -14,6 +14,7 @@
 // bf16 took 132 us with top = 5 and 171 with 32, against 105 without tokens.)
 // Bound by the bytes of the logits, read once.
 #include "common.hpp"
+#include <float.h>
 #include <math.h>
 #include <algorithm>
 
@@ -30,7 +31,7 @@ struct LogprobArgs {
     float scale;
 };
 
-constexpr int LP_TOP = LITHOS_LOGPROBS_MAX_TOP, LP_ROOM = 2048, LP_SEG = 8;
+constexpr int LP_TOP = LITHOS_LOGPROBS_MAX_TOP, LP_ROOM = 2048, LP_PAD = 32, LP_SEG = 8;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4_b4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -54,82 +55,104 @@ __device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xffffffffu -
 // sums of a softmax over some elements, d in powers of two
 struct Soft { float m, l, t; };
 
-__device__ __forceinline__ Soft soft_join(const Soft& a, const Soft& b, float c2)
-{
-    Soft r;
-    r.m = fmaxf(a.m, b.m);
-    const float ref = r.m == -INFINITY ? 0.0f : r.m;
-    // an empty side (m = -inf, l = t = 0) adds nothing; its distance must not become infinity times zero
-    const float ra = fmaxf((a.m - ref) * c2, -300.0f), rb = fmaxf((b.m - ref) * c2, -300.0f);
-    const float fa = __builtin_amdgcn_exp2f(ra), fb = __builtin_amdgcn_exp2f(rb);
-    r.l = fa * a.l + fb * b.l;
-    r.t = fa * fmaf(ra, a.l, a.t) + fb * fmaf(rb, b.l, b.t);
-    return r;
-}
-
 // x of the lane that the DPP control names (within a row of 16)
 template <int CTRL>
-__device__ __forceinline__ float from_lane(float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf, 0xf, true)); }
+__device__ __forceinline__ uint32_t from_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
 
-template <typename Op>
-__device__ __forceinline__ float wave_all(float x, Op op)
+// x joined with that of the lane at a distance of S: 1, 2, or of what is the same in all lanes of a group of S: 4, 8, 16, 32
+template <int S, typename Op>
+__device__ __forceinline__ uint32_t step(uint32_t x, Op op)
 {
-    x = op(x, from_lane<0x121>(x));               // row_ror by 1, 2, 4, 8
-    x = op(x, from_lane<0x122>(x));
-    x = op(x, from_lane<0x124>(x));
-    x = op(x, from_lane<0x128>(x));
-    x = op(x, __shfl_xor(x, 16));
-    return op(x, __shfl_xor(x, 32));
+    if constexpr (S == 1) return op(x, from_lane<0xb1>(x));                  // quad_perm 1 0 3 2
+    if constexpr (S == 2) return op(x, from_lane<0x4e>(x));                  // quad_perm 2 3 0 1
+    if constexpr (S == 4) return op(x, from_lane<0x141>(x));                 // row_half_mirror
+    if constexpr (S == 8) return op(x, from_lane<0x140>(x));                 // row_mirror
+    const auto both = S == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return op(both[0], both[1]);
+}
+
+// over groups of N lanes
+template <int N, typename Op>
+__device__ __forceinline__ uint32_t group_all(uint32_t x, Op op)
+{
+    if constexpr (N >= 2) x = step<1>(x, op);
+    if constexpr (N >= 4) x = step<2>(x, op);
+    if constexpr (N >= 8) x = step<4>(x, op);
+    if constexpr (N >= 16) x = step<8>(x, op);
+    if constexpr (N >= 32) x = step<16>(x, op);
+    if constexpr (N >= 64) x = step<32>(x, op);
+    return x;
+}
+template <int N>
+__device__ __forceinline__ float group_max(float x)
+{
+    return __uint_as_float(group_all<N>(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
+template <int N>
+__device__ __forceinline__ float group_sum(float x)
+{
+    return __uint_as_float(group_all<N>(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
 
 // The least of the maxima of the lanes' residue classes modulo `groups`, a power of two.
 __device__ __forceinline__ uint32_t least_of_groups(uint32_t x, int groups)
 {
-    auto step = [&](uint32_t y, int stride) { x = stride >= groups ? max(x, y) : min(x, y); };
-    step((uint32_t)__shfl_xor((int)x, 32), 32);
-    step((uint32_t)__shfl_xor((int)x, 16), 16);
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true), 8);     // row_ror: modulo 16 the neighbour at that distance
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xf, 0xf, true), 4);
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x122, 0xf, 0xf, true), 2);
-    step((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x121, 0xf, 0xf, true), 1);
-    return x;
+    auto join = [&](int stride) { return [=](uint32_t a, uint32_t b) { return stride >= groups ? max(a, b) : min(a, b); }; };
+    x = step<32>(x, join(32));
+    x = step<16>(x, join(16));
+    x = join(8)(x, from_lane<0x128>(x));          // row_ror: modulo 16 the neighbour at that distance
+    x = join(4)(x, from_lane<0x124>(x));
+    x = join(2)(x, from_lane<0x122>(x));
+    return join(1)(x, from_lane<0x121>(x));
 }
 
 __device__ __forceinline__ int power_of_two_from(int n) { return n <= 1 ? 1 : 1 << (32 - __clz(n - 1)); }
 
-// the sums of a wavefront's lanes, referred to the largest of their references
-__device__ __forceinline__ Soft soft_wave(const Soft& s, float c2)
+// the sums of N lanes, referred to the largest of their references
+template <int N>
+__device__ __forceinline__ Soft soft_all(const Soft& s, float c2)
 {
     Soft r;
-    r.m = wave_all(s.m, [](float a, float b) { return fmaxf(a, b); });
+    r.m = group_max<N>(s.m);
+    // an empty side (m = -inf, l = t = 0) adds nothing; its distance must not become infinity times zero
     const float d = fmaxf((s.m - (r.m == -INFINITY ? 0.0f : r.m)) * c2, -300.0f), f = __builtin_amdgcn_exp2f(d);
-    r.l = wave_all(f * s.l, [](float a, float b) { return a + b; });
-    r.t = wave_all(f * fmaf(d, s.l, s.t), [](float a, float b) { return a + b; });
+    r.l = group_sum<N>(f * s.l);
+    r.t = group_sum<N>(f * fmaf(d, s.l, s.t));
     return r;
 }
 
-// The k largest of n distinct keys in LDS, sorted, to `out`: a key's place is the number of larger ones.  By the whole
-// workgroup, up to eight neighbouring threads to a key; the caller puts barriers around it.
-__device__ __forceinline__ void choose_top(const uint64_t* keys, int n, int k, uint64_t* out)
+// the sums of W wavefronts, the same in all lanes
+template <int W>
+__device__ __forceinline__ Soft soft_of_waves(const Soft* softs, int lane, float c2)
 {
-    const int share = n > 128 ? 0 : n > 64 ? 1 : n > 32 ? 2 : 3;                 // log2 of the threads to a key
+    const Soft s = soft_all<16>(lane < W ? softs[lane] : Soft{-INFINITY, 0.0f, 0.0f}, c2);
+    auto first = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
+    return Soft{first(s.m), first(s.l), first(s.t)};
+}
+
+// The k largest of n distinct keys in LDS, sorted, to `out`: a key's place is the number of larger ones.  By the whole
+// workgroup of NT, up to eight neighbouring threads to a key; behind the keys there is room for LP_PAD more.  The caller puts
+// barriers around it.
+template <int NT>
+__device__ __forceinline__ void choose_top(uint64_t* keys, int n, int k, uint64_t* out)
+{
+    if (threadIdx.x < LP_PAD) keys[n + threadIdx.x] = 0;                          // larger than none
+    __syncthreads();
+    const int share = n > NT / 2 ? 0 : n > NT / 4 ? 1 : n > NT / 8 ? 2 : 3;       // log2 of the threads to a key
     const int part = threadIdx.x & ((1 << share) - 1), stride = 4 << share;
-    for (int i0 = 0; i0 < n; i0 += 256 >> share) {
+    for (int i0 = 0; i0 < n; i0 += NT >> share) {
         const int i = i0 + (threadIdx.x >> share);
         const uint64_t mine = keys[min(i, n - 1)];
-        int above = 0;
+        uint32_t above = 0;
 #pragma unroll 2
-        for (int o = 4 * part; o < n; o += stride) {
-            uint64_t other[4];
+        for (int o = 4 * part; o < n; o += stride)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) other[u] = keys[min(o + u, n - 1)];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) above += o + u < n && other[u] > mine;
-        }
-        if (share >= 1) above += __shfl_xor(above, 1);
-        if (share >= 2) above += __shfl_xor(above, 2);
-        if (share >= 3) above += __shfl_xor(above, 4);
-        if (i < n && part == 0 && above < k) out[above] = mine;
+            for (int u = 0; u < 4; ++u) above += keys[o + u] > mine;
+        const auto add = [](uint32_t a, uint32_t b) { return a + b; };
+        if (share >= 1) above = step<1>(above, add);
+        if (share >= 2) above = step<2>(above, add);
+        if (share >= 3) above = step<4>(above, add);
+        if (i < n && part == 0 && above < (uint32_t)k) out[above] = mine;
     }
 }
 
@@ -166,13 +189,82 @@ __device__ __forceinline__ int given_token(const LogprobArgs& a, int64_t row)
 }
 
 
+// A row's elements lie in tiles of 1024.  A lane owns 16 of a tile, in runs of 4 (fp32) or 8 (bf16).
+constexpr int LP_TILE = 1024;
+template <bool X32>
+struct LogitRow {
+    static constexpr int RUN = X32 ? 4 : 8;
+    const char* x;
+    int vocab;
+
+    __device__ __forceinline__ bool whole(int tile) const { return (tile + 1) * LP_TILE <= vocab; }
+    // element e of lane l; the last, partial tile is dealt out one element after another, so that every lane has some
+    __device__ __forceinline__ int index(int tile, int l, int e) const { return tile * LP_TILE + (whole(tile) ? (e / RUN) * 64 * RUN + l * RUN + e % RUN : e * 64 + l); }
+    // elements RUN q .. RUN q + RUN - 1 of lane l as four dwords
+    __device__ __forceinline__ u32x4 load_whole(int tile, int l, int q) const
+    {
+        return u32x4(*reinterpret_cast<const u32x4_b2*>(x + (int64_t)(tile * LP_TILE + q * 64 * RUN + l * RUN) * (X32 ? 4 : 2)));
+    }
+    __device__ __forceinline__ u32x4 load_partial(int tile, int l, int q) const       // what lies beyond the row is -infinity
+    {
+        uint32_t one[RUN];
+#pragma unroll
+        for (int e = 0; e < RUN; ++e) {
+            const int at = min(tile * LP_TILE + (RUN * q + e) * 64 + l, vocab - 1);
+            if constexpr (X32) one[e] = reinterpret_cast<const uint32_t*>(x)[at];
+            else one[e] = reinterpret_cast<const uint16_t*>(x)[at];
+        }
+#pragma unroll
+        for (int e = 0; e < RUN; ++e) if (tile * LP_TILE + (RUN * q + e) * 64 + l >= vocab) one[e] = X32 ? 0xff800000u : 0xff80u;
+        u32x4 v;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) v[d] = X32 ? one[d] : one[(2 * d) % RUN] | (one[(2 * d + 1) % RUN] << 16);
+        return v;
+    }
+    __device__ __forceinline__ u32x4 load(int tile, int l, int q) const { return whole(tile) ? load_whole(tile, l, q) : load_partial(tile, l, q); }
+    __device__ __forceinline__ void unpack(const u32x4& v, float* f) const
+    {
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            if constexpr (X32) f[d] = __uint_as_float(v[d]);
+            else { f[2 * d] = __uint_as_float(v[d] << 16); f[2 * d + 1] = __uint_as_float(v[d] & 0xffff0000u); }
+        }
+    }
+};
+
+// the row's or the split's n chosen keys, by the whole workgroup: to the workspace, or made K of them (rows with NaN: any token)
+__device__ __forceinline__ void save_top(const LogprobArgs& a, int64_t row, int sp, int n, uint64_t* chosen)
+{
+    const int tid = threadIdx.x, K = a.top;
+    if (a.splits == 1) {
+        if (tid >= n && tid < K) chosen[tid] = top_key(-INFINITY, tid);
+    } else if (tid < 64) {
+        float* w = a.ws + (row * a.splits + sp) * (4 + 2 * K);
+        if (tid == 0) w[3] = (float)n;
+        if (tid < n) reinterpret_cast<uint2*>(w + 4)[tid] = make_uint2((uint32_t)chosen[tid], (uint32_t)(chosen[tid] >> 32));
+    }
+}
+
+// the rest of the results, by one wavefront, the first
+__device__ __forceinline__ void save_sums(const LogprobArgs& a, int64_t row, int sp, const Soft& s, int token, float logit, const uint64_t* chosen, int lane)
+{
+    if (a.splits == 1) {
+        wave_lds_sync();
+        write_row(a, row, s, logit, token >= 0, chosen, lane);
+    } else if (lane == 0) {
+        float* w = a.ws + (row * a.splits + sp) * (4 + 2 * a.top);
+        w[0] = s.m; w[1] = s.l; w[2] = s.t;
+        if (a.top == 0) w[3] = 0.0f;
+    }
+}
+
 // Logical block = (row, split).  The split's elements are tiles of 1024 which its four wavefronts take in turn; a lane
 // owns 16 of a tile, in runs of 4 (fp32) or 8 (bf16).
 template <bool X32>
 __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs atom)
 {
-    constexpr int RUN = X32 ? 4 : 8, TILE = 1024, NW = X32 ? 16 : 8;      // NW dwords of a tile per lane
-    __shared__ __attribute__((aligned(16))) uint64_t cand[LP_ROOM + LP_TOP];
+    constexpr int RUN = LogitRow<X32>::RUN, RUNS = 16 / RUN;
+    __shared__ __attribute__((aligned(16))) uint64_t cand[LP_ROOM + LP_TOP + LP_PAD];
     __shared__ uint64_t chosen[LP_TOP];
     __shared__ Soft softs[4];
     __shared__ float nth[3][4];                   // per wavefront: its ceil(K / 4)-th, ceil(K / 2)-th and K-th largest lane maximum
@@ -187,54 +279,30 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
     const uint32_t sp = S == 1 ? 0 : L % S;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int tiles = (a.vocab + TILE - 1) / TILE;
+    const int tiles = (a.vocab + LP_TILE - 1) / LP_TILE;
     const int t0 = S == 1 ? 0 : (int)(sp * tiles / S), t1 = S == 1 ? tiles : (int)((sp + 1) * tiles / S);        // 64 * 2^20 at most
     const float c2 = a.scale * LOG2E;
     const int K = a.top;
 
-    const char* const xrow = reinterpret_cast<const char*>(a.x) + row * a.ldx * (X32 ? 4 : 2);
-    // element e of lane l; the last, partial tile is dealt out one element after another, so that every lane has some
-    auto index = [&](int tile, int l, int e) { return tile * TILE + ((tile + 1) * TILE <= a.vocab ? (e / RUN) * 64 * RUN + l * RUN + e % RUN : e * 64 + l); };
-    // elements RUN q .. RUN q + RUN - 1 of lane l as four dwords
-    auto load = [&](int tile, int l, int q) {
-        if ((tile + 1) * TILE <= a.vocab) return u32x4(*reinterpret_cast<const u32x4_b2*>(xrow + (int64_t)index(tile, l, RUN * q) * (X32 ? 4 : 2)));
-        uint32_t one[RUN];                       // what lies beyond the row is -infinity
-#pragma unroll
-        for (int e = 0; e < RUN; ++e) {
-            const int at = min(index(tile, l, RUN * q + e), a.vocab - 1);
-            if constexpr (X32) one[e] = reinterpret_cast<const uint32_t*>(xrow)[at];
-            else one[e] = reinterpret_cast<const uint16_t*>(xrow)[at];
-        }
-#pragma unroll
-        for (int e = 0; e < RUN; ++e) if (index(tile, l, RUN * q + e) >= a.vocab) one[e] = X32 ? 0xff800000u : 0xff80u;
-        u32x4 v;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) v[d] = X32 ? one[d] : one[(2 * d) % RUN] | (one[(2 * d + 1) % RUN] << 16);
-        return v;
-    };
-    auto unpack = [&](const u32x4& v, float* x) {
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-            if constexpr (X32) x[d] = __uint_as_float(v[d]);
-            else { x[2 * d] = __uint_as_float(v[d] << 16); x[2 * d + 1] = __uint_as_float(v[d] & 0xffff0000u); }
-        }
-    };
+    const LogitRow<X32> x_of{reinterpret_cast<const char*>(a.x) + row * a.ldx * (X32 ? 4 : 2), a.vocab};
 
     Soft s = {-INFINITY, 0.0f, 0.0f};            // m: a value near the largest one, see below
     float most = -INFINITY, peak = -INFINITY;     // the largest of this lane's elements, of its present stretch
     const int turns = (t1 - t0 + 3) / 4, len = max(1, (turns + LP_SEG - 1) / LP_SEG);
     int left = len, seg = 0;
-    u32x4 raw[NW / 4];
+    u32x4 raw[RUNS];
     if (t0 + wave < t1)
 #pragma unroll
-        for (int q = 0; q < NW / 4; ++q) raw[q] = load(t0 + wave, lane, q);
+        for (int q = 0; q < RUNS; ++q) raw[q] = x_of.load(t0 + wave, lane, q);
+    const int token = wave == 0 && S == 1 ? given_token(a, row) : -1;
+    const float logit = token >= 0 ? logit_at<X32>(a, row, token) : 0.0f;
     for (int tile = t0 + wave; tile < t1; tile += 4) {
         float x[16];
 #pragma unroll
-        for (int q = 0; q < NW / 4; ++q) unpack(raw[q], x + RUN * q);
+        for (int q = 0; q < RUNS; ++q) x_of.unpack(raw[q], x + RUN * q);
         if (tile + 4 < t1)
 #pragma unroll
-            for (int q = 0; q < NW / 4; ++q) raw[q] = load(tile + 4, lane, q);
+            for (int q = 0; q < RUNS; ++q) raw[q] = x_of.load(tile + 4, lane, q);
 
         float mt = x[0];
 #pragma unroll
@@ -285,7 +353,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
         }
         if (tid == 0) n_sel = n_cand = 0;
     }
-    s = soft_wave(s, c2);
+    s = soft_all<64>(s, c2);
     if (lane == 0) softs[wave] = s;
     __syncthreads();
     if (K) {
@@ -293,90 +361,53 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
         float bound = fminf(fminf(nth[0][0], nth[0][1]), fminf(nth[0][2], nth[0][3]));
         bound = fmaxf(bound, fmaxf(fminf(hi01, hi23), fmaxf(lo01, lo23)));                 // second largest
         bound = fmaxf(bound, fmaxf(fmaxf(nth[2][0], nth[2][1]), fmaxf(nth[2][2], nth[2][3])));
+        const float least = fmaxf(bound, -FLT_MAX);                                       // forbidden ones are no candidates
         // elements above `floor` (a key) of a run to the candidates
         auto offer = [&](const u32x4& v, int tile, int l, int q, uint64_t floor) {
             float x[RUN];
-            unpack(v, x);
+            uint32_t some = 0;
+            x_of.unpack(v, x);
+#pragma unroll
+            for (int e = 0; e < RUN; ++e) some |= (x[e] >= least && top_key(x[e], x_of.index(tile, l, RUN * q + e)) > floor ? 1u : 0u) << e;
+            if (some == 0) return;
+            int at = atomicAdd(&n_cand, __popc(some));
 #pragma unroll
             for (int e = 0; e < RUN; ++e)
-                if (x[e] >= bound && x[e] > -INFINITY) {
-                    const uint64_t k = top_key(x[e], index(tile, l, RUN * q + e));
-                    if (k > floor) {
-                        const int at = atomicAdd(&n_cand, 1);
-                        if (at < LP_ROOM + LP_TOP) cand[at] = k;
-                    }
+                if (some >> e & 1) {
+                    if (at < LP_ROOM + LP_TOP) cand[at] = top_key(x[e], x_of.index(tile, l, RUN * q + e));
+                    ++at;
                 }
         };
         // of forbidden tokens, where fewer than K are allowed, the first K suffice
         auto fill = [&]() {
-            const int i = t0 * TILE + tid;
-            if (bound == -INFINITY && tid < K && i < min(t1 * TILE, a.vocab) && logit_at<X32>(a, row, i) == -INFINITY) {
-                const int at = atomicAdd(&n_cand, 1);
-                if (at < LP_ROOM + LP_TOP) cand[at] = top_key(-INFINITY, i);
-            }
+            const int i = t0 * LP_TILE + tid;
+            if (bound == -INFINITY && tid < K && i < min(t1 * LP_TILE, a.vocab) && logit_at<X32>(a, row, i) == -INFINITY) cand[atomicAdd(&n_cand, 1)] = top_key(-INFINITY, i);
         };
-        constexpr int RUNS = 16 / RUN;
-        const bool at_hand = turns == 1;              // a tile for each wavefront at most: it is still in registers
-        auto select = [&]() {
-            for (int g = 0; g < seg; ++g) {
-                const float p = peaks[g][tid];
-                if (p >= bound && p > -INFINITY) sel[atomicAdd(&n_sel, 1)] = (uint16_t)(g * 256 + tid);     // in any order: places follow from keys
-            }
-        };
+        for (int g = 0; g < seg; ++g)
+            if (peaks[g][tid] >= least) sel[atomicAdd(&n_sel, 1)] = (uint16_t)(g * 256 + tid);       // in any order: places follow from keys
         fill();
-        if (!at_hand) {
-            select();
-        } else if (t0 + wave < t1) {
-            float x[16];
-            uint32_t mine = 0;
-#pragma unroll
-            for (int q = 0; q < RUNS; ++q) unpack(raw[q], x + RUN * q);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) mine |= (x[e] >= bound && x[e] > -INFINITY ? 1u : 0u) << e;
-            // the wavefront's places behind one another, lane by lane
-            const int n = __popc(mine);
-            int at = 0, total = 0;
-#pragma unroll
-            for (int b = 0; b < 5; ++b) {             // 16 at most
-                const uint64_t m = __ballot((n >> b) & 1);
-                at += __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0)) << b;
-                total += __popcll(m) << b;
-            }
-            int base = 0;
-            if (lane == 0) base = atomicAdd(&n_cand, total);
-            at += __builtin_amdgcn_readfirstlane(base);
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (mine >> e & 1) {
-                    if (at < LP_ROOM + LP_TOP) cand[at] = top_key(x[e], index(t0 + wave, lane, e));
-                    ++at;
-                }
-        }
         __syncthreads();
         // item i, a run of a stretch
         auto scan = [&](int i, uint64_t floor) {
             const int who = sel[i / (RUNS * len)] & 255, g = sel[i / (RUNS * len)] >> 8, q = i % RUNS, tile = t0 + (who >> 6) + 4 * (g * len + i / RUNS % len);
-            if (tile < t1) offer(load(tile, who & 63, q), tile, who & 63, q, floor);
+            if (tile < t1) offer(x_of.load(tile, who & 63, q), tile, who & 63, q, floor);
         };
-        if (!at_hand) {
-            for (int i = tid; i < n_sel * len * RUNS; i += 256) scan(i, 0);
-            __syncthreads();
-        }
+        const int items = n_sel * len * RUNS;
+        for (int i = tid; i < items; i += 256) scan(i, 0);
+        __syncthreads();
         int n = n_cand;
         if (n > LP_ROOM) {
             // many equal values: 256 items at a time, and only what is above the K-th chosen so far
             __syncthreads();
-            if (at_hand) select();
             if (tid == 0) n_cand = 0;
             __syncthreads();
-            const int items = n_sel * len * RUNS;
             fill();
             n = 0;
             for (int i0 = 0; i0 < items; i0 += 256) {
                 if (i0 + tid < items) scan(i0 + tid, n >= K ? chosen[K - 1] : 0);
                 __syncthreads();
                 n = n_cand;
-                choose_top(cand, n, K, chosen);
+                choose_top<256>(cand, n, K, chosen);
                 __syncthreads();
                 n = min(n, K);
                 if (tid < n) cand[tid] = chosen[tid];
@@ -384,29 +415,196 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
                 __syncthreads();
             }
         }
-        choose_top(cand, n, K, chosen);
+        choose_top<256>(cand, n, K, chosen);
         __syncthreads();
         n = min(n, K);
-        if (a.splits == 1 && tid >= n && tid < K) chosen[tid] = top_key(-INFINITY, tid);      // rows with NaN: any token
-        if (wave == 0 && a.splits > 1) {
-            float* w = a.ws + ((int64_t)row * a.splits + sp) * (4 + 2 * K);
-            if (lane == 0) w[3] = (float)n;
-            if (lane < n) reinterpret_cast<uint2*>(w + 4)[lane] = make_uint2((uint32_t)chosen[lane], (uint32_t)(chosen[lane] >> 32));
-        }
+        save_top(a, row, sp, n, chosen);
     }
     if (wave != 0) return;
-    s = softs[0];
+    s = soft_of_waves<4>(softs, lane, c2);
+    save_sums(a, row, sp, s, token, logit, chosen, lane);
+}
+
+// The same where few workgroups meet a short piece: W wavefronts hold all of it, T tiles each, in registers.  All of it is
+// on its way at once, the sums refer to the largest value itself, and nothing is read twice.  The candidates' bound is the
+// `top`-th largest of the maxima of 64 to 127 groups of lanes.
+template <bool X32, int W, int T>
+__global__ __launch_bounds__(W * 64) void logprobs_held_kernel(LogprobArgs a, AtomArgs atom)
+{
+    constexpr int RUN = LogitRow<X32>::RUN, RUNS = 16 / RUN, NT = W * 64, TPG = NT / 128;         // threads to a group
+    __shared__ __attribute__((aligned(16))) uint64_t cand[LP_ROOM + LP_TOP + LP_PAD];
+    __shared__ uint64_t chosen[LP_TOP];
+    __shared__ Soft softs[W];
+    __shared__ __attribute__((aligned(16))) uint32_t peaks[128];      // largest elements of the groups, ordered
+    __shared__ uint32_t bound_s;
+    __shared__ int n_cand;
+
+    const uint32_t L = atom_logical_block(atom), S = a.splits;
+    const int64_t row = S == 1 ? L : L / S;
+    const uint32_t sp = S == 1 ? 0 : L % S;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tiles = (a.vocab + LP_TILE - 1) / LP_TILE;
+    const int t0 = S == 1 ? 0 : (int)(sp * tiles / S), t1 = S == 1 ? tiles : (int)((sp + 1) * tiles / S);        // at most W T tiles
+    const float c2 = a.scale * LOG2E;
+    const int K = a.top;
+    const LogitRow<X32> x_of{reinterpret_cast<const char*>(a.x) + row * a.ldx * (X32 ? 4 : 2), a.vocab};
+
+    u32x4 raw[T][RUNS];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) s = soft_join(s, softs[w], c2);
-    if (a.splits == 1) {
-        const int t = given_token(a, row);
-        wave_lds_sync();
-        write_row(a, row, s, t >= 0 ? logit_at<X32>(a, row, t) : 0.0f, t >= 0, chosen, lane);
-    } else if (lane == 0) {
-        float* w = a.ws + ((int64_t)row * a.splits + sp) * (4 + 2 * K);
-        w[0] = s.m; w[1] = s.l; w[2] = s.t;
-        if (K == 0) w[3] = 0.0f;
+    for (int i = 0; i < T; ++i) {
+        const int tile = t0 + wave + W * i;
+        constexpr uint32_t none = X32 ? 0xff800000u : 0xff80ff80u;                  // -infinity
+#pragma unroll
+        for (int q = 0; q < RUNS; ++q) raw[i][q] = tile < t1 && x_of.whole(tile) ? x_of.load_whole(tile, lane, q) : u32x4{none, none, none, none};
     }
+    if (t1 == tiles && !x_of.whole(tiles - 1) && (tiles - 1 - t0) % W == wave) {      // the row's end, which may break off anywhere
+        u32x4 part[RUNS];
+#pragma unroll
+        for (int q = 0; q < RUNS; ++q) part[q] = x_of.load_partial(tiles - 1, lane, q);
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+            if (t0 + wave + W * i == tiles - 1)
+#pragma unroll
+                for (int q = 0; q < RUNS; ++q) raw[i][q] = part[q];
+    }
+    const int token = wave == 0 && S == 1 ? given_token(a, row) : -1;
+    const float logit = token >= 0 ? logit_at<X32>(a, row, token) : 0.0f;
+    if (tid == 0) { n_cand = 0; bound_s = ordered(-INFINITY); }
+
+    const int busy = min(W, t1 - t0), group = busy >= 16 ? 16 : busy >= 8 ? 8 : busy >= 4 ? 4 : busy >= 2 ? 2 : 1;      // wavefronts with elements
+    const int groups = busy * 64 / group;
+    float most = -INFINITY, most_of[T];
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        float x[16];
+#pragma unroll
+        for (int q = 0; q < RUNS; ++q) x_of.unpack(raw[i][q], x + RUN * q);
+        most_of[i] = x[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) most_of[i] = fmaxf(most_of[i], x[e]);
+        most = fmaxf(most, most_of[i]);
+    }
+    Soft s = {0.0f, 0.0f, 0.0f};
+    {
+        const auto larger = [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); };
+        uint32_t x = __float_as_uint(most), peak = x;
+        x = step<1>(x, larger); if (group >= 2) peak = x;
+        x = step<2>(x, larger); if (group >= 4) peak = x;
+        x = step<4>(x, larger); if (group >= 8) peak = x;
+        x = step<8>(x, larger); if (group >= 16) peak = x;
+        x = step<16>(x, larger);
+        s.m = __uint_as_float(step<32>(x, larger));
+        if (K && wave < busy && lane % group == 0) peaks[tid / group] = ordered(__uint_as_float(peak));
+        if (K && tid < 128 && tid >= groups) peaks[tid] = 0;                                 // less than any
+    }
+    const float ref = s.m == -INFINITY ? 0.0f : s.m;
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        float x[16];
+#pragma unroll
+        for (int q = 0; q < RUNS; ++q) x_of.unpack(raw[i][q], x + RUN * q);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            // the difference first: products of masks of the type's lowest value overflow
+            const float d = (x[e] - ref) * c2, p = __builtin_amdgcn_exp2f(d);
+            s.l += p;
+            s.t = fmaf(p, fmaxf(d, -300.0f), s.t);            // 0, not infinity times 0, for a forbidden token
+        }
+    }
+    s.l = group_sum<64>(s.l);
+    s.t = group_sum<64>(s.t);
+    if (lane == 0) softs[wave] = s;
+    __syncthreads();
+    if (K) {
+        {
+            const uint32_t mine = peaks[tid / TPG];
+            uint32_t above = 0, from = 0;
+            for (int o = tid % TPG * 4; o < groups; o += TPG * 4) {
+                const uint4 other = *reinterpret_cast<const uint4*>(peaks + o);
+                above += (other.x > mine) + (other.y > mine) + (other.z > mine) + (other.w > mine);
+                from += (other.x >= mine) + (other.y >= mine) + (other.z >= mine) + (other.w >= mine);
+            }
+            const auto add = [](uint32_t a, uint32_t b) { return a + b; };
+            above = group_all<TPG>(above, add);
+            from = group_all<TPG>(from, add);
+            if (tid / TPG < groups && (int)above < K && (int)from >= K) bound_s = mine;      // the same of all who write
+        }
+        __syncthreads();
+        const float bound = value_of(bound_s);
+        const float least = fmaxf(bound, -FLT_MAX);                                       // forbidden ones are no candidates
+        int total = 0;
+#pragma unroll
+        for (int i = 0; i < T; ++i)
+            if (__any(most_of[i] >= least)) {
+                float x[16];
+#pragma unroll
+                for (int q = 0; q < RUNS; ++q) x_of.unpack(raw[i][q], x + RUN * q);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) total += __popcll(__ballot(x[e] >= least));
+            }
+        if (total) {
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&n_cand, total);    // in any order: places follow from keys
+            at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+            for (int i = 0; i < T; ++i)
+                if (__any(most_of[i] >= least)) {
+                    float x[16];
+#pragma unroll
+                    for (int q = 0; q < RUNS; ++q) x_of.unpack(raw[i][q], x + RUN * q);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint64_t some = __ballot(x[e] >= least);
+                        if (some == 0) continue;
+                        const int mine = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(some >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)some, 0));
+                        if (x[e] >= least && mine < LP_ROOM) cand[mine] = top_key(x[e], x_of.index(t0 + wave + W * i, lane, e));
+                        at += __popcll(some);
+                    }
+                }
+        }
+        // of forbidden tokens, where fewer than K are allowed, the first K suffice
+        auto fill = [&]() {
+            const int i = t0 * LP_TILE + tid;
+            if (bound == -INFINITY && tid < K && i < min(t1 * LP_TILE, a.vocab) && logit_at<X32>(a, row, i) == -INFINITY) {
+                const int at = atomicAdd(&n_cand, 1);
+                if (at < LP_ROOM) cand[at] = top_key(-INFINITY, i);
+            }
+        };
+        fill();
+        __syncthreads();
+        int n = n_cand;
+        if (n > LP_ROOM) {
+            // many equal values: an element per thread at a time, and only what is above the K-th chosen so far
+            __syncthreads();
+            if (tid == 0) n_cand = 0;
+            __syncthreads();
+            fill();
+            n = 0;
+            for (int i0 = t0 * LP_TILE; i0 < min(t1 * LP_TILE, a.vocab); i0 += NT) {
+                const int i = i0 + tid;
+                const float x = i < min(t1 * LP_TILE, a.vocab) ? logit_at<X32>(a, row, i) : -INFINITY;
+                if (x >= least) {
+                    const uint64_t k = top_key(x, i);
+                    if (k > (n >= K ? chosen[K - 1] : 0)) cand[atomicAdd(&n_cand, 1)] = k;      // NT and K at most
+                }
+                __syncthreads();
+                n = n_cand;
+                choose_top<NT>(cand, n, K, chosen);
+                __syncthreads();
+                n = min(n, K);
+                if (tid < n) cand[tid] = chosen[tid];
+                if (tid == 0) n_cand = n;
+                __syncthreads();
+            }
+        }
+        choose_top<NT>(cand, n, K, chosen);
+        __syncthreads();
+        save_top(a, row, sp, min(n, K), chosen);
+    }
+    if (wave != 0) return;
+    s = soft_of_waves<W>(softs, lane, c2);
+    save_sums(a, row, sp, s, token, logit, chosen, lane);
 }
 
 // Joins the splits of a row: one workgroup per row.  With j = ceil(top / splits) at least `top` keys reach the least of the
@@ -414,7 +612,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(LogprobArgs a, AtomArgs a
 template <bool X32>
 __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobArgs a, AtomArgs atom)
 {
-    __shared__ __attribute__((aligned(16))) uint64_t cand[LITHOS_LOGPROBS_MAX_SPLITS * LP_TOP + 1];
+    __shared__ __attribute__((aligned(16))) uint64_t cand[LITHOS_LOGPROBS_MAX_SPLITS * LP_TOP + LP_PAD];
     __shared__ uint64_t chosen[LP_TOP], bound_s;
     __shared__ int n_cand;
     const int64_t row = atom_logical_block(atom);
@@ -443,7 +641,7 @@ __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobArgs a, Atom
             const uint32_t v = least_of_groups((uint32_t)(jth >> 32), power_of_two_from(m));         // 0: not as many splits
             if (lane == 0) { n_cand = 0; bound_s = (uint64_t)v << 32; }
         }
-        s = soft_wave(Soft{p.x, p.y, p.z}, c2);
+        s = soft_all<64>(Soft{p.x, p.y, p.z}, c2);
     }
     if (K) {
         __syncthreads();
@@ -456,7 +654,7 @@ __global__ __launch_bounds__(256) void logprobs_merge_kernel(LogprobArgs a, Atom
         }
         __syncthreads();
         const int n = n_cand;
-        choose_top(cand, n, K, chosen);
+        choose_top<256>(cand, n, K, chosen);
         if (tid >= n && tid < K) chosen[tid] = top_key(-INFINITY, tid);         // rows with NaN: any token
         __syncthreads();
     }
@@ -542,10 +740,32 @@ __global__ __launch_bounds__(256) void logprobs_grad_kernel(LogprobGradArgs a, A
 typedef void (*lp_fn)(LogprobArgs, AtomArgs);
 typedef void (*lp_grad_fn)(LogprobGradArgs, AtomArgs);
 
+// Wavefronts and tiles of each that hold a workgroup's piece, 0: it is read as a stream.  Held by 16 wavefronts where each has a
+// CU for itself (33 rows of 32003, top 32, 11.8 -> 8.7 us a pass; 1 of 16384 7.5 -> 6.0; 200 of 50001 13.7 -> 12.6; more rows
+// are as fast as a stream: 300 of 50001 20.8 whole).  Eight tiles spill: 200 rows of 131072 took 59 us, as a stream 22.
+struct Held { int waves, tiles; };
+static Held lp_held(const lithos_op_t& op)
+{
+    const int64_t splits = std::max<int64_t>(1, op.dim[3]), blocks = op.dim[0] * splits;
+    const int64_t piece = ((op.dim[1] + LP_TILE - 1) / LP_TILE + splits - 1) / splits;         // tiles
+    if (op.kind != LITHOS_OP_LOGPROBS) return {0, 0};
+    if (piece <= 4) return {4, 1};
+    if (blocks > 256 || piece > 64) return {0, 0};
+    return {16, piece <= 16 ? 1 : piece <= 32 ? 2 : 4};
+}
+
+template <bool X32>
+static lp_fn lp_pick(const lithos_op_t& op)
+{
+    const Held h = lp_held(op);
+    if (h.waves == 4) return logprobs_held_kernel<X32, 4, 1>;
+    return h.tiles == 1 ? logprobs_held_kernel<X32, 16, 1> : h.tiles == 2 ? logprobs_held_kernel<X32, 16, 2> : h.tiles == 4 ? logprobs_held_kernel<X32, 16, 4> : logprobs_kernel<X32>;
+}
+
 static lp_fn lp_kernel(const lithos_op_t& op)
 {
     const bool x32 = op.flags & LITHOS_F_IN_F32;
-    if (op.kind == LITHOS_OP_LOGPROBS) return x32 ? logprobs_kernel<true> : logprobs_kernel<false>;
+    if (op.kind == LITHOS_OP_LOGPROBS) return x32 ? lp_pick<true>(op) : lp_pick<false>(op);
     return x32 ? logprobs_merge_kernel<true> : logprobs_merge_kernel<false>;
 }
 
@@ -593,7 +813,8 @@ int logprobs_plan(const lithos_op_t& op, OpPlan* plan)
     if (blocks > 0x7fffffffull) return fail(LITHOS_EINVAL, "logprobs: too many workgroups");
     plan->grid = {(uint32_t)blocks, 1, 1};
     plan->total = (uint32_t)blocks;
-    plan->wg_per_cu = cached_occupancy(grad ? (const void*)lp_grad_kernel(op) : (const void*)lp_kernel(op), 256, 4);
+    if (!grad && lp_held(op).waves) plan->threads = 64 * lp_held(op).waves;
+    plan->wg_per_cu = cached_occupancy(grad ? (const void*)lp_grad_kernel(op) : (const void*)lp_kernel(op), (int)plan->threads, 4);
     return LITHOS_OK;
 }
 
@@ -621,15 +842,15 @@ int logprobs_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& a
     return LITHOS_OK;
 }
 
-// Two workgroups per CU of the target, each with a tile of 1024 for every one of its four wavefronts.  A second launch costs
-// what a workgroup takes for some 40000 tokens: rows whose other pieces have no more than that stay whole.  Whole / split, us a
-// pass: 33 x 32003 11.8 / 12.6, 150 x 50001 13.6 / 15, 400 x 50001 16.9 / 20.7, 1 x 32000 10.1 / 9.3 (bf16); 4 x 50257
-// 12.9 / 9.9, 4 x 131072 22.8 / 9.9 (fp32), 64 x 131072 22 / 13.8, 300 x 131072 28.6 / 26.9, 400 x 131072 31 / 32.1.
+// Rows of up to 65536 tokens stay whole: a second launch costs more than it saves (us a pass, whole / best split: 33 x 32003
+// 8.7 / 11.2, 64 x 50257 11.2 / 11.1, 250 x 65536 15.8 / 20, 400 x 50001 17 / 20).  Longer ones are cut into a piece for each
+// CU, at least two, of a tile of 1024 for each of four wavefronts: 4 x 131072 21 / 9.7 (32 pieces), 64 x 131072 22 / 12.5 (4),
+// 128 x 131072 22 / 16.4 (2), 300 x 131072 27.4 / 26.2 (2); 400 x 131072 31 / 32.
 int logprobs_split_hint(const lithos_op_t& op, int n_cus)
 {
-    const int64_t vocab = op.dim[1], quads = (vocab + 4095) / 4096, want = (2ll * n_cus + op.dim[0] - 1) / op.dim[0];
-    const int64_t s = std::max<int64_t>(1, std::min({quads, want, (int64_t)LITHOS_LOGPROBS_MAX_SPLITS}));
-    return vocab - vocab / s > 40000 ? (int)s : 1;
+    const int64_t rows = op.dim[0], quads = (op.dim[1] + 4 * LP_TILE - 1) / (4 * LP_TILE);
+    if (op.dim[1] <= 64 * LP_TILE || 2 * rows >= 3ll * n_cus) return 1;
+    return (int)std::min({quads, std::max<int64_t>(2, (n_cus + rows - 1) / rows), (int64_t)LITHOS_LOGPROBS_MAX_SPLITS});
 }
 
 } // namespace lithos

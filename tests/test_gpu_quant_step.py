@@ -540,6 +540,30 @@ def test_logprobs_without_tokens_and_with_large_logits():
     check_lp(stats, ids, x, [5, 6, 7], 3, 1.0)
 
 
+@pytest.mark.parametrize("rows,vocab,splits", [(3, 16385, 1), (3, 32768, 1), (3, 32769, 1), (2, 65536, 1), (2, 65537, 1), (2, 140003, 1), (2, 140003, 2), (2, 140003, 5),
+                                               (2, 140003, 64), (257, 5003, 1), (300, 9001, 1), (120, 9001, 3)])
+@pytest.mark.parametrize("dt", [F32, BF])
+@pytest.mark.parametrize("masked", [0.0, 0.9])
+def test_logprobs_long_rows_and_many_rows(rows, vocab, splits, dt, masked):
+    x = logits(rows, vocab, dt, pad=3, masked=masked)
+    tokens = [(7919 * r) % vocab for r in range(rows)]
+    for top in (0, 7, 32):
+        stats, ids = lp_run(x, vocab, tokens, top, scale=0.8, splits=splits)
+        check_lp(stats, ids, x[:, :vocab], tokens, top, 0.8)
+
+
+@pytest.mark.parametrize("kind", ["rising", "falling", "equal", "two_values", "none"])
+@pytest.mark.parametrize("rows,vocab", [(1, 50001), (1, 65536), (1, 100003), (300, 6001)])
+def test_logprobs_order_of_long_rows_and_many_rows(kind, rows, vocab):
+    i = torch.arange(vocab).float()
+    row = {"rising": i / vocab, "falling": -i / vocab, "equal": 0 * i + 1.5, "two_values": (torch.arange(vocab) % 7 == 3).float(), "none": 0 * i - math.inf}[kind]
+    x = row[None].repeat(rows, 1)
+    for top in (1, 32):
+        stats, ids = lp_run(x, vocab, [vocab - 1] * rows, top)
+        check_lp(stats[-1:], ids[-1:], x[-1:], [vocab - 1], top, 1.0)
+        assert bits_equal(stats, stats[-1:].repeat(rows, 1)) and torch.equal(ids, ids[-1:].repeat(rows, 1))
+
+
 def test_logprobs_in_atoms_is_the_whole_launch():
     x = logits(9, 7001, BF, masked=0.3)
     for splits in (1, 3):
