@@ -149,8 +149,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, AtomAr
             for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
         }
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    top = lane_group<64>(top, [](uint32_t x, uint32_t y) { return max(x, y); });
     if constexpr (WPU == 4) {
         if (lane == 0) tops[wave] = top;
         __syncthreads();
@@ -410,8 +409,8 @@ __global__ __launch_bounds__(W * 64, 2) void attn_dec8_kernel(Dec8Args a, AtomAr
         float bm = s8[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) bm = fmaxf(bm, s8[i]);
-        bm = fmaxf(bm, __shfl_xor(bm, 16));
-        bm = fmaxf(bm, __shfl_xor(bm, 32));
+        const auto larger = [](uint32_t x, uint32_t y) { return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y))); };
+        bm = __uint_as_float(lane_step<32>(lane_step<16>(__float_as_uint(bm), larger), larger));
         // the reference follows the largest score once that is 2^8 times as likely: nothing is lost, and few units pay for it
         if (__any(bm > m + 8.0f)) {
             const float nm = fmaxf(m, bm);

@@ -143,6 +143,34 @@ __device__ __forceinline__ float gelu_erf(float u)
     return fabsf(u) < 1.25f ? near : far;
 }
 
+// x of the lane that the DPP control names (within a row of 16)
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_from(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
+
+// x joined with that of the lane at a distance of S; 4 and 8: of an x that is the same in all lanes of a group of S
+template <int S, typename Op>
+__device__ __forceinline__ uint32_t lane_step(uint32_t x, Op op)
+{
+    if constexpr (S == 1) return op(x, lane_from<0xb1>(x));                  // quad_perm 1 0 3 2
+    if constexpr (S == 2) return op(x, lane_from<0x4e>(x));                  // quad_perm 2 3 0 1
+    if constexpr (S == 4) return op(x, lane_from<0x141>(x));                 // row_half_mirror
+    if constexpr (S == 8) return op(x, lane_from<0x140>(x));                 // row_mirror
+    const auto both = S == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return op(both[0], both[1]);
+}
+
+// over groups of N lanes
+template <int N, typename Op>
+__device__ __forceinline__ uint32_t lane_group(uint32_t x, Op op)
+{
+    if constexpr (N >= 2) x = lane_step<1>(x, op);
+    if constexpr (N >= 4) x = lane_step<2>(x, op);
+    if constexpr (N >= 8) x = lane_step<4>(x, op);
+    if constexpr (N >= 16) x = lane_step<8>(x, op);
+    if constexpr (N >= 32) x = lane_step<16>(x, op);
+    if constexpr (N >= 64) x = lane_step<32>(x, op);
+    return x;
+}
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned_to(const void* p, unsigned bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }      // null is
 

@@ -55,55 +55,27 @@ __device__ __forceinline__ uint32_t key_index(uint64_t k) { return 0xffffffffu -
 // sums of a softmax over some elements, d in powers of two
 struct Soft { float m, l, t; };
 
-// x of the lane that the DPP control names (within a row of 16)
-template <int CTRL>
-__device__ __forceinline__ uint32_t from_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
-
-// x joined with that of the lane at a distance of S: 1, 2, or of what is the same in all lanes of a group of S: 4, 8, 16, 32
-template <int S, typename Op>
-__device__ __forceinline__ uint32_t step(uint32_t x, Op op)
-{
-    if constexpr (S == 1) return op(x, from_lane<0xb1>(x));                  // quad_perm 1 0 3 2
-    if constexpr (S == 2) return op(x, from_lane<0x4e>(x));                  // quad_perm 2 3 0 1
-    if constexpr (S == 4) return op(x, from_lane<0x141>(x));                 // row_half_mirror
-    if constexpr (S == 8) return op(x, from_lane<0x140>(x));                 // row_mirror
-    const auto both = S == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return op(both[0], both[1]);
-}
-
-// over groups of N lanes
-template <int N, typename Op>
-__device__ __forceinline__ uint32_t group_all(uint32_t x, Op op)
-{
-    if constexpr (N >= 2) x = step<1>(x, op);
-    if constexpr (N >= 4) x = step<2>(x, op);
-    if constexpr (N >= 8) x = step<4>(x, op);
-    if constexpr (N >= 16) x = step<8>(x, op);
-    if constexpr (N >= 32) x = step<16>(x, op);
-    if constexpr (N >= 64) x = step<32>(x, op);
-    return x;
-}
 template <int N>
 __device__ __forceinline__ float group_max(float x)
 {
-    return __uint_as_float(group_all<N>(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+    return __uint_as_float(lane_group<N>(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
 }
 template <int N>
 __device__ __forceinline__ float group_sum(float x)
 {
-    return __uint_as_float(group_all<N>(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+    return __uint_as_float(lane_group<N>(__float_as_uint(x), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
 
 // The least of the maxima of the lanes' residue classes modulo `groups`, a power of two.
 __device__ __forceinline__ uint32_t least_of_groups(uint32_t x, int groups)
 {
     auto join = [&](int stride) { return [=](uint32_t a, uint32_t b) { return stride >= groups ? max(a, b) : min(a, b); }; };
-    x = step<32>(x, join(32));
-    x = step<16>(x, join(16));
-    x = join(8)(x, from_lane<0x128>(x));          // row_ror: modulo 16 the neighbour at that distance
-    x = join(4)(x, from_lane<0x124>(x));
-    x = join(2)(x, from_lane<0x122>(x));
-    return join(1)(x, from_lane<0x121>(x));
+    x = lane_step<32>(x, join(32));
+    x = lane_step<16>(x, join(16));
+    x = join(8)(x, lane_from<0x128>(x));          // row_ror: modulo 16 the neighbour at that distance
+    x = join(4)(x, lane_from<0x124>(x));
+    x = join(2)(x, lane_from<0x122>(x));
+    return join(1)(x, lane_from<0x121>(x));
 }
 
 __device__ __forceinline__ int power_of_two_from(int n) { return n <= 1 ? 1 : 1 << (32 - __clz(n - 1)); }
@@ -149,9 +121,9 @@ __device__ __forceinline__ void choose_top(uint64_t* keys, int n, int k, uint64_
 #pragma unroll
             for (int u = 0; u < 4; ++u) above += keys[o + u] > mine;
         const auto add = [](uint32_t a, uint32_t b) { return a + b; };
-        if (share >= 1) above = step<1>(above, add);
-        if (share >= 2) above = step<2>(above, add);
-        if (share >= 3) above = step<4>(above, add);
+        if (share >= 1) above = lane_step<1>(above, add);
+        if (share >= 2) above = lane_step<2>(above, add);
+        if (share >= 3) above = lane_step<4>(above, add);
         if (i < n && part == 0 && above < (uint32_t)k) out[above] = mine;
     }
 }
@@ -489,12 +461,12 @@ __global__ __launch_bounds__(W * 64) void logprobs_held_kernel(LogprobArgs a, At
     {
         const auto larger = [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); };
         uint32_t x = __float_as_uint(most), peak = x;
-        x = step<1>(x, larger); if (group >= 2) peak = x;
-        x = step<2>(x, larger); if (group >= 4) peak = x;
-        x = step<4>(x, larger); if (group >= 8) peak = x;
-        x = step<8>(x, larger); if (group >= 16) peak = x;
-        x = step<16>(x, larger);
-        s.m = __uint_as_float(step<32>(x, larger));
+        x = lane_step<1>(x, larger); if (group >= 2) peak = x;
+        x = lane_step<2>(x, larger); if (group >= 4) peak = x;
+        x = lane_step<4>(x, larger); if (group >= 8) peak = x;
+        x = lane_step<8>(x, larger); if (group >= 16) peak = x;
+        x = lane_step<16>(x, larger);
+        s.m = __uint_as_float(lane_step<32>(x, larger));
         if (K && wave < busy && lane % group == 0) peaks[tid / group] = ordered(__uint_as_float(peak));
         if (K && tid < 128 && tid >= groups) peaks[tid] = 0;                                 // less than any
     }
@@ -526,8 +498,8 @@ __global__ __launch_bounds__(W * 64) void logprobs_held_kernel(LogprobArgs a, At
                 from += (other.x >= mine) + (other.y >= mine) + (other.z >= mine) + (other.w >= mine);
             }
             const auto add = [](uint32_t a, uint32_t b) { return a + b; };
-            above = group_all<TPG>(above, add);
-            from = group_all<TPG>(from, add);
+            above = lane_group<TPG>(above, add);
+            from = lane_group<TPG>(from, add);
             if (tid / TPG < groups && (int)above < K && (int)from >= K) bound_s = mine;      // the same of all who write
         }
         __syncthreads();
