@@ -25,7 +25,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // that is at least s_new; otherwise its earlier codes c become round(fl(fl(c s_old) / s_new)).  New codes are
 // round(fl(x / s)), 0 where s is 0 or no number.  Every step is an IEEE fp32 operation, so the result is defined to the bit.
 // Bound by the bytes of the new rows and codes; 64 rows of fp32 or 128 of bf16 stay in registers between the maximum
-// and the codes, longer blocks are read twice.  A lane owns eight neighbouring elements of a row: 16-byte loads (two of them
+// and the codes, longer blocks are read twice: 8192 tokens of 8 heads of 128 bf16 take 12.9 us, 3.9 TB/s.  A lane owns eight neighbouring elements of a row: 16-byte loads (two of them
 // for fp32), 8-byte stores.
 struct Kv8AppendArgs {
     const void* x[2];           // new keys, new values: row (b * T + t), head h at column h * d
@@ -201,7 +201,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, AtomAr
 // two (2^-16) for bf16.  The 16 columns hold CS heads (4, 8 or 16, the group rounded up) of 16 / CS planes, so that a
 // group of up to four heads takes one product where 16 heads take one per plane; the planes' scores are added across the
 // columns, and the accumulators at the end.  Scale factors are applied to sums and probabilities in fp32; exponents are
-// powers of two.
+// powers of two.  Measured: 8 sequences of 32768 keys, 8 heads of 64, in 56 us (4.8 TB/s), 16 ragged ones of up to 2049 keys,
+// 8 heads of 128, in 13.6 us (34 MB; an empty launch takes 3), one of 300 keys in 7.4 us.
 struct Dec8Args {
     const void* q;
     const uint8_t* k;
@@ -543,7 +544,9 @@ static dec8_fn dec8_group(const lithos_op_t& op)
     return G <= 4 ? dec8_pick<D, 4, W>(e, q, o) : G <= 8 ? dec8_pick<D, 8, W>(e, q, o) : dec8_pick<D, 16, W>(e, q, o);
 }
 
-static int dec8_waves(const lithos_op_t& op) { return op.dim[0] * op.dim[2] * std::max<int64_t>(1, op.dim[6]) > 256 ? 4 : 8; }
+// Four / eight wavefronts, us a pass with the merge: 16 ragged sequences, 8 heads of 128, whole (128 blocks) 19.9 / 18.9, 4 splits
+// 16.9 / 22.1; 32 sequences of 512 keys, whole (256 blocks) 11.3 / 12.1; 8 of 32768, heads of 64, 4 splits 77 / 69, 8 splits 62 / 65.
+static int dec8_waves(const lithos_op_t& op) { return op.dim[0] * op.dim[2] * std::max<int64_t>(1, op.dim[6]) >= 256 ? 4 : 8; }
 
 static dec8_fn dec8_kernel(const lithos_op_t& op)
 {
@@ -551,7 +554,8 @@ static dec8_fn dec8_kernel(const lithos_op_t& op)
     return op.dim[3] == 64 ? dec8_group<64, 8>(op) : dec8_group<128, 8>(op);
 }
 
-// A workgroup per block for more than 16 tokens: 8192 bf16 tokens of 8 heads of 128 took 23.9 us with a wavefront per block.
+// A workgroup per block for more than 16 tokens: 8192 bf16 tokens of 8 heads of 128 take 17.4 us with blocks of 32 positions,
+// 21.5 with a wavefront per block, 64 tokens 5.3 and 8.5; one token 5.5 and 5.2.
 static int append_waves(const lithos_op_t& op) { return op.dim[1] > 16 ? 4 : 1; }
 
 template <int D, int WPU>
@@ -669,16 +673,17 @@ int kv8_launch(const lithos_op_t& op, const OpPlan& plan, const AtomArgs& atom, 
 }
 
 // Key ranges per (sequence, key/value head).  One CU fetches some 27 bytes a nanosecond, and a launch with its merge costs
-// about 4 us: up to 128 KB a workgroup stays alone (1 sequence of 8 heads, 512 keys 9 us whole).  Beyond, ranges of at least
-// a unit for each wavefront, as many as the chip holds at a time: two workgroups of four wavefronts on a CU (heads of 64:
-// four), or, where that would be more than eight ranges to merge, one of eight.
+// about 4 us: up to 128 KB a workgroup stays alone (8 heads of 128, whole / 2 / 4 / 8 splits, us a pass: 300 keys 7.3, 10.8, 10.0,
+// 9.7, 512 keys 9.3, 11.3, 10.0, 9.5, 1024 keys 12.6, 13.7, 11.2, 9.9).  Beyond, ranges of at least 128 keys, a unit for each
+// of four wavefronts, as many as the chip holds at a time: two workgroups of four wavefronts on a CU (heads of 64: four), or,
+// where that would be more than eight ranges to merge, one of eight (16 ragged sequences 2, 4, 8 splits 18.0, 16.9, 20.5).
 int kv8_split_hint(const lithos_op_t& op, int n_cus)
 {
     const int64_t bytes = 2 * op.dim[3] * op.dim[4], pairs = op.dim[0] * op.dim[2], per_cu = op.dim[3] == 64 ? 4 : 2;
     if (bytes <= 128 * 1024) return 1;
     int64_t s = per_cu * n_cus / pairs;
     if (s > 8) s = std::max<int64_t>(8, per_cu / 2 * n_cus / pairs);
-    return (int)std::max<int64_t>(1, std::min({s, ceil_div(op.dim[4], 256), (int64_t)LITHOS_ATTN_MAX_SPLITS}));
+    return (int)std::max<int64_t>(1, std::min({s, ceil_div(op.dim[4], 128), (int64_t)LITHOS_ATTN_MAX_SPLITS}));
 }
 
 } // namespace lithos

@@ -14,7 +14,10 @@ static int q4_rows(const lithos_op_t& op)
 }
 
 // 16-column blocks per workgroup.  More blocks share the loads and the splitting of A, which weigh about as much as x blocks;
-// fewer fill the chip.  Time goes with rounds of workgroups times blocks + x.  A value of C does not depend on the choice.
+// fewer fill the chip.  Time goes with the workgroups of a CU times blocks + x.  A value of C does not depend on the choice.
+// Eight blocks of up to four rows are 12 % slower than four (1 x 2 x 14336 x 4096: 1, 2, 4, 8 blocks 19.5, 19.7, 18.0, 20.3 us
+// a pass); 8 rows 30, 30, 25.5, 22.8, 16 rows 42, 42, 31.7, 26.5; 1 x 4096 x 4096 5.5, 6.2, 8.1, 12.7, 1 x 6144 x 4096 7.2, 6.5,
+// 8.3, 12.8; 24 x 5003 x 2088 bf16 10.6, 8.7, 12.1.
 static int q4_blocks(const lithos_op_t& op)
 {
     const bool glu = op.flags & LITHOS_F_GLU, a32 = op.flags & LITHOS_F_IN_F32;
@@ -22,9 +25,8 @@ static int q4_blocks(const lithos_op_t& op)
     const int64_t tiles = (glu ? 2 : 1) * ((op.dim[1] + 15) / 16), gy = (op.dim[0] + rows - 1) / rows;
     int best = 0;
     int64_t least = 0;
-    for (int nb = glu ? 2 : 1; nb <= (rows == 32 ? 4 : 8); nb *= 2) {
-        const int64_t groups = (tiles + nb - 1) / nb * gy, room = 256 * q4_resident(rows, nb, a32);
-        const int64_t t = (groups + room - 1) / room * q4_resident(rows, nb, a32) * (nb + x);
+    for (int nb = glu ? 2 : 1; nb <= (rows <= 4 || rows == 32 ? 4 : 8); nb *= 2) {
+        const int64_t t = ((tiles + nb - 1) / nb * gy + 255) / 256 * (nb + x);
         if (!best || t < least) { best = nb; least = t; }
     }
     return best;

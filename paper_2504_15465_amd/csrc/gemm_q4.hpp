@@ -16,6 +16,8 @@
 // in wavefront order.  sum_k A of a group is one more product, with a column operand of ones, so it comes out in the
 // accumulators' layout.  Scales and zero points come four groups of all tiles at a time, one 16-byte load per lane, and
 // pass through the wavefront's own piece of LDS (a load of their own for each tile and chunk took as long as the codes).
+// Measured: 1 x 4096 x 4096 in 4.9 us, 8 rows against 2 x 14336 x 4096 with gated SiLU in 20.6 us (66 MB, 3.2 TB/s: the rows,
+// 128 KB for each of 224 workgroups, weigh a third of what a CU fetches), 27 x 5003 x 2088 bf16 in 9.0 us.
 #pragma once
 #include "gemm_common.hpp"
 
@@ -259,12 +261,13 @@ void gemm_q4_kernel(GemmQ4Args a, AtomArgs atom)
 
 typedef void (*gemm_q4_fn)(GemmQ4Args, AtomArgs);
 
-// rows: 2, 4, 8, 16 (fp32), 4, 16, 32 (bf16); blocks: 1, 2, 4, 8 (32 rows: at most 4)
+// rows: 2, 4, 8, 16 (fp32), 4, 16, 32 (bf16); blocks: 1, 2, 4, 8 (2, 4 and 32 rows: at most 4)
 template <int GS, int NB>
 static gemm_q4_fn q4_pick(int rows, bool a32)
 {
-    if (!a32) return rows == 4 ? gemm_q4_kernel<4, NB, GS, false> : rows == 16 ? gemm_q4_kernel<16, NB, GS, false> : gemm_q4_kernel<32, NB == 8 ? 4 : NB, GS, false>;
-    return rows == 2 ? gemm_q4_kernel<2, NB, GS, true> : rows == 4 ? gemm_q4_kernel<4, NB, GS, true>
+    constexpr int FEW = NB == 8 ? 4 : NB;
+    if (!a32) return rows == 4 ? gemm_q4_kernel<4, FEW, GS, false> : rows == 16 ? gemm_q4_kernel<16, NB, GS, false> : gemm_q4_kernel<32, FEW, GS, false>;
+    return rows == 2 ? gemm_q4_kernel<2, FEW, GS, true> : rows == 4 ? gemm_q4_kernel<4, FEW, GS, true>
          : rows == 8 ? gemm_q4_kernel<8, NB, GS, true> : gemm_q4_kernel<16, NB, GS, true>;
 }
 
