@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8AppendArgs a, AtomAr
 // group of up to four heads takes one product where 16 heads take one per plane; the planes' scores are added across the
 // columns, and the accumulators at the end.  Scale factors are applied to sums and probabilities in fp32; exponents are
 // powers of two.  Measured: 8 sequences of 32768 keys, 8 heads of 64, in 56 us (4.8 TB/s), 16 ragged ones of up to 2049 keys,
-// 8 heads of 128, in 13.6 us (34 MB; an empty launch takes 3), one of 300 keys in 7.4 us.
+// 8 heads of 128, in 14 us (34 MB; an empty launch takes 3), one of 300 keys in 7.4 us.
 struct Dec8Args {
     const void* q;
     const uint8_t* k;
