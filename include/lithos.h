@@ -147,6 +147,7 @@ enum {
  *             / 448) of what is appended to it; if the block holds earlier positions and its scale is larger, that stays, and if
  *             smaller, the earlier codes are rounded to the new one (code = round(code * old / new)).  Codes are round(x / scale),
  *             to nearest even, in fp32 quotients.  A block that receives a NaN or an infinity reads as NaN.
+ *             Appends to one sequence, and the attention that reads it, follow one another on a queue.
  * ATTN_DEC8   batch,n_q,n_kv,d,keys,cap,splits,block   q,kcodes,vcodes,[workspace],scales,[lens(i32)] / o   ld0=q row stride;
  *             like ATTN_DEC, against KV8_APPEND's cache (E4M3 as there); 1 to 16 query heads per key/value head,    fparam0=scale
  *             d = 64 or 128.  lens: keys of each sequence, at most `keys` (what is beyond counts as `keys`); a sequence of none
@@ -158,6 +159,7 @@ enum {
  *             id.  top <= 32.  A row without an allowed token: log-sum-exp and log probabilities -infinity, entropy 0; a
  *             row with a NaN or +infinity: NaN, and any ids of the vocabulary.  splits > 1 cuts every row into ranges whose
  *             partial results go to the workspace, rows*splits*(4 + 2 top) floats, and LOGPROBS_MERGE on the same queue joins them.
+ *             Launches that may overlap need a workspace each (ATTN_DEC8's likewise).
  * LOGPROBS_MERGE rows,vocab,top,splits           logits,[tokens],workspace / stats,[ids]   as LOGPROBS
  * LOGPROBS_GRAD rows,vocab                       logits,[tokens],stats,[g_logprob(f32)],[g_entropy(f32)] / dlogits   ld0=of logits,
  *             dlogits = d(sum g_logprob*logprob + g_entropy*entropy) / d logits (bf16, fp32 with OUT_F32); stats are         ld1=of stats,

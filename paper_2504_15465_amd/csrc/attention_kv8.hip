@@ -25,8 +25,8 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // that is at least s_new; otherwise its earlier codes c become round(fl(fl(c s_old) / s_new)).  New codes are
 // round(fl(x / s)), 0 where s is 0 or no number.  Every step is an IEEE fp32 operation, so the result is defined to the bit.
 // Bound by the bytes of the new rows and codes; 64 rows of fp32 or 128 of bf16 stay in registers between the maximum
-// and the codes, longer blocks are read twice: 8192 tokens of 8 heads of 128 bf16 take 12.9 us, 3.9 TB/s.  A lane owns eight neighbouring elements of a row: 16-byte loads (two of them
-// for fp32), 8-byte stores.
+// and the codes, longer blocks are read twice: 8192 tokens of 8 heads of 128 bf16 take 12.9 us, 3.9 TB/s.  A lane owns eight
+// neighbouring elements of a row: 16-byte loads (two of them for fp32), 8-byte stores.
 struct Kv8AppendArgs {
     const void* x[2];           // new keys, new values: row (b * T + t), head h at column h * d
     uint8_t* codes[2];
