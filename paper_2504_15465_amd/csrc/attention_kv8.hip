@@ -56,7 +56,7 @@ __device__ __forceinline__ uint32_t encode4(const float (&y)[8], int at)
 // codes of eight elements.  The quotient by a scale of ordinary size takes two corrections with its rounded reciprocal: the
 // first leaves it within one unit of the last place, the second, whose remainder is exact, rounds it correctly (P. Markstein,
 // 1990), in five instructions where the division takes eleven.  Elements so small that a remainder would not be exact have
-// code 0 either way.
+// code 0 either way.  (The remainder is s y - x, not x - s y: for x = -0 the latter would add +0 and lose the sign, which e4m3 keeps.)
 template <bool E4M3>
 __device__ __forceinline__ uint2 quantise8(const float (&x)[8], float s, float rcp)
 {
@@ -65,8 +65,8 @@ __device__ __forceinline__ uint2 quantise8(const float (&x)[8], float s, float r
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             y[e] = x[e] * rcp;
-            y[e] = fmaf(fmaf(-s, y[e], x[e]), rcp, y[e]);
-            y[e] = fmaf(fmaf(-s, y[e], x[e]), rcp, y[e]);
+            y[e] = fmaf(fmaf(s, y[e], -x[e]), -rcp, y[e]);
+            y[e] = fmaf(fmaf(s, y[e], -x[e]), -rcp, y[e]);
         }
     } else {
 #pragma unroll
