@@ -134,15 +134,16 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t row, con
 {
     const float ln = logf(s.l);
     const bool none = s.m == -INFINITY && s.l == 0.0f;          // no token is allowed
+    const bool broken = s.l != s.l;                             // a NaN or +infinity in the row: that decides before a -infinity does
     float* st = a.stats + row * a.lds;
     if (lane == 0) {
-        st[0] = !given ? 0.0f : logit == -INFINITY ? -INFINITY : a.scale * (logit - s.m) - ln;
+        st[0] = !given ? 0.0f : logit == -INFINITY && !broken ? -INFINITY : a.scale * (logit - s.m) - ln;
         st[1] = none ? 0.0f : ln - s.t * LN2 / s.l;
         st[2] = none ? -INFINITY : fmaf(a.scale, s.m, ln);
     }
     if (lane < a.top) {
         const float x = key_value(top[lane]);
-        st[3 + lane] = x == -INFINITY ? -INFINITY : a.scale * (x - s.m) - ln;
+        st[3 + lane] = x == -INFINITY && !broken ? -INFINITY : a.scale * (x - s.m) - ln;
         a.ids[row * a.ldi + lane] = (int32_t)key_index(top[lane]);
     }
 }
