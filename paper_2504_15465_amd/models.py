@@ -220,6 +220,8 @@ class DecoderChain:
     ``q4_group`` (32, 64 or 128) quantises the weights to 4 bits in groups of as many k: the RMSNorms are then
     launches of their own.  ``kv8_block`` (a multiple of 16) keeps the cache in 8 bits (int8, or e4m3 with
     ``kv8_e4m3``) with a scale per block of as many positions and head; the given prompt is quantised into it here.
+    Where ``pos`` lies inside a block, a step quantises the prompt's part of that block anew before it appends (one
+    more launch per layer), since an append may coarsen the block for good: a step's answer depends on its input alone.
     ``head``: ``dict(rms=[H], w=[H, V] weight bits)`` makes the step end in the answer: logits, and in ``stats``
     (log probability of ``tokens``, entropy, log-sum-exp, ``top`` log probabilities) and ``ids`` what LOGPROBS says of them."""
 
@@ -243,7 +245,7 @@ class DecoderChain:
         for L in layers:
             self.w.append(dict(rms1=_f32(L["rms1"], device), rms2=_f32(L["rms2"], device),
                                w_qkv=weight(L["w_qkv"]), w_o=weight(L["w_o"]), w_gu=weight(L["w_gu"]), w_d=weight(L["w_d"])))
-        self.kc, self.vc, self.kv_scales = [], [], []
+        self.kc, self.vc, self.kv_scales, self.kv_open = [], [], [], []      # kv_open: the prompt's rows in the block of `pos`
         if kv8_block:
             self._quantise_cache(kcache_bits, vcache_bits, device, torch.float8_e4m3fn if kv8_e4m3 else torch.int8, ctx)
         else:
@@ -294,6 +296,9 @@ class DecoderChain:
                 scales = torch.zeros((2, batch, -(-self.cap // block), n_kv), dtype=torch.float32, device=device)
                 if self.pos:
                     k, v = _dev(kb, device), _dev(vb, device)
+                    first = self.pos // block * block
+                    if first < self.pos:
+                        self.kv_open.append(tuple(x[:, first:].contiguous() for x in (k, v)))
                     torch.cuda.synchronize(device)
                     B.lithos_launch_atomized(ctx, B.kv8_append_op(k, v, kc, vc, scales, batch, self.pos, n_kv, d, 0, self.cap, block))
                     B.lithos_partition_sync(ctx)
@@ -328,9 +333,13 @@ class DecoderChain:
                         _product(self.n, W["w_qkv"], self.qkv, Bn, nqkv, H)]
             if self.kv8_block:
                 kv = self.qkv[:, n_q * d:]
-                ops += [B.rope_kv_op(self.qkv, None, None, Bn, n_q, n_kv, d, self.pos, self.cap),
-                        B.kv8_append_op(kv, kv[:, n_kv * d:], self.kc[li], self.vc[li], self.kv_scales[li], Bn, 1, n_kv, d, self.pos,
-                                        self.cap, self.kv8_block, ldx=nqkv)]
+                ops.append(B.rope_kv_op(self.qkv, None, None, Bn, n_q, n_kv, d, self.pos, self.cap))
+                if self.kv_open:
+                    k, v = self.kv_open[li]
+                    ops.append(B.kv8_append_op(k, v, self.kc[li], self.vc[li], self.kv_scales[li], Bn, k.shape[1], n_kv, d, self.pos - k.shape[1],
+                                               self.cap, self.kv8_block))
+                ops.append(B.kv8_append_op(kv, kv[:, n_kv * d:], self.kc[li], self.vc[li], self.kv_scales[li], Bn, 1, n_kv, d, self.pos,
+                                           self.cap, self.kv8_block, ldx=nqkv))
             else:
                 ops.append(B.rope_kv_op(self.qkv, self.kc[li], self.vc[li], Bn, n_q, n_kv, d, self.pos, self.cap))
             ops.append(self._attention(li, S, self.ws if S > 1 else None))
