@@ -260,10 +260,23 @@ def attn_merge_op(workspace, o, batch, n_q, n_kv, d, splits, op_id=0) -> Op:
     return make_op(OP_ATTN_MERGE, (batch, n_q, n_kv, d, splits), flags, inputs=(workspace,), outputs=(o,), op_id=op_id)
 
 
+_REAL = (torch.float32, torch.bfloat16)
+_CODES = (torch.int8, torch.float8_e4m3fn)
+
+
+def _types(who, **args):
+    """The library reads bare pointers: a tensor of another type would be taken for what it is not.  ``args``: (tensor, its types)."""
+    for name, (t, dtypes) in args.items():
+        if isinstance(t, torch.Tensor) and t.dtype not in dtypes:
+            raise ValueError("%s: %s must be %s (got %s)" % (who, name, " or ".join(str(d)[6:] for d in dtypes), str(t.dtype)[6:]))
+
+
 def gemm_q4_op(a, codes, scales, c, m, n, k, group, zeros=None, bias=None, gelu=False, residual=None, glu=False,
                lda=None, ldc=None, ldr=None, op_id=0) -> Op:
     """Weights in 4 bits as ``quant.pack_q4`` lays them out, ``scales`` and ``zeros`` (None: 8) as ``quant.pack_q4_groups`` does;
     ``glu``: they have 2n rows, gate rows then up rows, and ``c`` = silu(gate product) * (up product)."""
+    _types("gemm_q4", a=(a, _REAL), codes=(codes, (torch.uint8, torch.int8)), scales=(scales, (torch.bfloat16,)), zeros=(zeros, (torch.bfloat16,)),
+           bias=(bias, (torch.float32,)), residual=(residual, (torch.float32,)), c=(c, _REAL))
     flags = (F_BIAS if bias is not None else 0) | (F_GELU if gelu else 0) | (F_RESIDUAL if residual is not None else 0) | (F_GLU if glu else 0)
     flags |= (F_IN_F32 if a.dtype == torch.float32 else 0) | (F_OUT_F32 if c.dtype == torch.float32 else 0)
     return make_op(OP_GEMM_Q4, (m, n, k, group), flags,
@@ -274,6 +287,8 @@ def gemm_q4_op(a, codes, scales, c, m, n, k, group, zeros=None, bias=None, gelu=
 def kv8_append_op(k, v, kcodes, vcodes, scales, batch, tokens, n_kv, d, pos, cap, block, positions=None, ldx=None, op_id=0) -> Op:
     """Quantise ``tokens`` new keys and values per sequence into the cache, from position ``pos`` (or ``positions[b]``) on.
     ``kcodes`` and ``vcodes`` are [batch, cap, n_kv, d] int8 or float8_e4m3fn, ``scales`` fp32 [2, batch, ceil(cap / block), n_kv]."""
+    _types("kv8_append", k=(k, _REAL), v=(v, (k.dtype,)), kcodes=(kcodes, _CODES), vcodes=(vcodes, (kcodes.dtype,)), scales=(scales, (torch.float32,)),
+           positions=(positions, (torch.int32,)))
     flags = (F_IN_F32 if k.dtype == torch.float32 else 0) | (F_E4M3 if kcodes.dtype == torch.float8_e4m3fn else 0)
     return make_op(OP_KV8_APPEND, (batch, tokens, n_kv, d, pos, cap, block), flags, ld=(ldx if ldx is not None else n_kv * d,),
                    inputs=(k, v, positions, scales), outputs=(kcodes, vcodes), op_id=op_id)
@@ -283,6 +298,8 @@ def attn_dec8_op(q, kcodes, vcodes, scales, o, batch, n_q, n_kv, d, keys, cap, b
                  splits=1, workspace=None) -> Op:
     """Decode attention against a cache of ``kv8_append_op``; ``lens``: int32 keys per sequence (None: ``keys`` everywhere).
     splits > 1 needs an fp32 workspace of attn_workspace_floats(...) elements and an attn_merge_op after it."""
+    _types("attn_dec8", q=(q, _REAL), kcodes=(kcodes, _CODES), vcodes=(vcodes, (kcodes.dtype,)), scales=(scales, (torch.float32,)), o=(o, _REAL),
+           lens=(lens, (torch.int32,)), workspace=(workspace, (torch.float32,)))
     flags = (F_IN_F32 if q.dtype == torch.float32 else 0) | (F_OUT_F32 if o.dtype == torch.float32 else 0)
     flags |= F_E4M3 if kcodes.dtype == torch.float8_e4m3fn else 0
     return make_op(OP_ATTN_DEC8, (batch, n_q, n_kv, d, keys, cap, splits, block), flags, ld=(ldq if ldq is not None else n_q * d,),
@@ -294,6 +311,8 @@ def logprobs_workspace_floats(rows, top, splits) -> int:
 
 
 def _logprobs(kind, logits, tokens, stats, ids, rows, vocab, top, splits, workspace, scale, ldx, lds, ldi, op_id) -> Op:
+    _types("logprobs", logits=(logits, _REAL), tokens=(tokens, (torch.int32,)), workspace=(workspace, (torch.float32,)), stats=(stats, (torch.float32,)),
+           ids=(ids, (torch.int32,)))
     return make_op(kind, (rows, vocab, top, splits), F_IN_F32 if logits.dtype == torch.float32 else 0,
                    ld=(ldx if ldx is not None else vocab, lds if lds is not None else 3 + top, ldi if ldi is not None else top),
                    fparam=(scale,), inputs=(logits, tokens, workspace), outputs=(stats, ids), op_id=op_id)
@@ -313,6 +332,8 @@ def logprobs_merge_op(workspace, logits, tokens, stats, ids, rows, vocab, top, s
 
 def logprobs_grad_op(logits, tokens, stats, g_logprob, g_entropy, dlogits, rows, vocab, scale=1.0, ldx=None, lds=None, ldd=None, op_id=0) -> Op:
     """Gradient of sum(g_logprob * log probability + g_entropy * entropy) with respect to the logits (None: zeros)."""
+    _types("logprobs_grad", logits=(logits, _REAL), tokens=(tokens, (torch.int32,)), stats=(stats, (torch.float32,)), g_logprob=(g_logprob, (torch.float32,)),
+           g_entropy=(g_entropy, (torch.float32,)), dlogits=(dlogits, _REAL))
     flags = (F_IN_F32 if logits.dtype == torch.float32 else 0) | (F_OUT_F32 if dlogits.dtype == torch.float32 else 0)
     lds = lds if lds is not None else stats.shape[-1]
     return make_op(OP_LOGPROBS_GRAD, (rows, vocab), flags, ld=(ldx if ldx is not None else vocab, lds, ldd if ldd is not None else vocab),
