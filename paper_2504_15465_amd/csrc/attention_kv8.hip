@@ -618,6 +618,7 @@ int kv8_plan(const lithos_op_t& op, OpPlan* plan)
         if (!op.in[2] && (pos < 0 || pos > cap - T)) return fail(LITHOS_EINVAL, "kv8_append: positions %lld .. %lld lie outside the cache", (long long)pos, (long long)(pos + T - 1));
         if (!op.in[0] || !op.in[1] || !op.in[3] || !op.out[0] || !op.out[1]) return fail(LITHOS_EINVAL, "kv8_append: null operand");
         const bool x32 = op.flags & LITHOS_F_IN_F32;
+        if (op.flags & ~(LITHOS_F_IN_F32 | LITHOS_F_E4M3)) return fail(LITHOS_EINVAL, "kv8_append: takes IN_F32 and E4M3 only");
         if (!aligned16(op.in[0]) || !aligned16(op.in[1]) || !aligned16(op.out[0]) || !aligned16(op.out[1]))
             return fail(LITHOS_EINVAL, "kv8_append: keys, values and caches must be 16-byte aligned");
         if (!aligned_to(op.in[2], 4) || !aligned_to(op.in[3], 4)) return fail(LITHOS_EINVAL, "kv8_append: misaligned positions or scales");
@@ -636,6 +637,7 @@ int kv8_plan(const lithos_op_t& op, OpPlan* plan)
     const int rc = check_cache("attn_dec8", batch, n_kv, d, cap, block);
     if (rc != LITHOS_OK) return rc;
     if (n_q <= 0 || n_q % n_kv || n_q / n_kv > 16) return fail(LITHOS_EINVAL, "attn_dec8: need 1 to 16 query heads per key/value head (got %lld and %lld)", (long long)n_q, (long long)n_kv);
+    if (op.flags & ~(LITHOS_F_IN_F32 | LITHOS_F_OUT_F32 | LITHOS_F_E4M3)) return fail(LITHOS_EINVAL, "attn_dec8: takes IN_F32, OUT_F32 and E4M3 only");
     if (keys <= 0 || keys > cap) return fail(LITHOS_EINVAL, "attn_dec8: need 0 < keys <= cap");
     if (op.ld[0] < n_q * d) return fail(LITHOS_EINVAL, "attn_dec8: q row stride smaller than n_q*d");
     if (!op.in[0] || !op.in[1] || !op.in[2] || !op.in[4] || !op.out[0]) return fail(LITHOS_EINVAL, "attn_dec8: null operand");

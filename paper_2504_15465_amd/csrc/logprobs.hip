@@ -758,6 +758,8 @@ int logprobs_plan(const lithos_op_t& op, OpPlan* plan)
     const bool grad = op.kind == LITHOS_OP_LOGPROBS_GRAD, x32 = op.flags & LITHOS_F_IN_F32;
     if (rows <= 0 || vocab <= 0 || rows > (1ll << 31) - 1 || vocab > (1ll << 30))
         return fail(LITHOS_EINVAL, "logprobs: rows and vocabulary must be positive (got %lld, %lld)", (long long)rows, (long long)vocab);
+    if (op.flags & ~(LITHOS_F_IN_F32 | (grad ? LITHOS_F_OUT_F32 : 0u)))
+        return fail(LITHOS_EINVAL, grad ? "logprobs_grad: takes IN_F32 and OUT_F32 only" : "logprobs: takes IN_F32 only");
     if (!(op.fparam[0] > 0.0f) || !(op.fparam[0] < INFINITY)) return fail(LITHOS_EINVAL, "logprobs: the scale (fparam0) must be positive and finite");
     if (op.ld[0] < vocab) return fail(LITHOS_EINVAL, "logprobs: row stride of the logits smaller than the vocabulary");
     if (!op.in[0] || reinterpret_cast<uintptr_t>(op.in[0]) % (x32 ? 4 : 2)) return fail(LITHOS_EINVAL, "logprobs: null or misaligned logits");
