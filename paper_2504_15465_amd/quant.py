@@ -21,10 +21,11 @@ def quantize_q4(w: torch.Tensor, group: int, symmetric: bool = False):
         zero = torch.full_like(scale, 8.0)
     else:
         lo = torch.where(live, x, torch.inf).amin(2)
-        scale = (torch.where(live, x, -torch.inf).amax(2) - lo) / 15.0
-        # equal weights: one step away from zero each, so that code and zero point reproduce them
-        scale = torch.where(scale > 0, scale, torch.where(lo != 0, lo.abs(), 1.0))
-        zero = (-lo / scale.bfloat16().float()).bfloat16().float()
+        scale = ((torch.where(live, x, -torch.inf).amax(2) - lo) / 15.0).bfloat16()
+        # weights that are equal, or less apart than bf16 can say: one step away from zero, so that code and zero point reproduce them
+        for other in (lo.abs().bfloat16(), torch.ones_like(scale)):
+            scale = torch.where(scale > 0, scale, other)
+        zero = (-lo / scale.float()).bfloat16().float()
     scale = scale.bfloat16()
     s = scale.float()
     q = torch.where(s[:, :, None] > 0, x / s[:, :, None], 0.0) + zero[:, :, None]
