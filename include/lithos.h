@@ -159,7 +159,7 @@ enum {
  *             id.  top <= 32.  A row without an allowed token: log-sum-exp and log probabilities -infinity, entropy 0; a
  *             row with a NaN or +infinity: NaN everywhere (0 still for no given token), and any ids of the vocabulary.
  *             splits > 1 cuts every row into ranges whose partial results go to the workspace, rows*splits*(4 + 2 top)
- *             floats, and LOGPROBS_MERGE on the same queue joins them.
+ *             floats, and LOGPROBS_MERGE on the same queue joins them.  0 < scale < 2.3e38.
  *             Launches that may overlap need a workspace each (ATTN_DEC8's likewise).
  * LOGPROBS_MERGE rows,vocab,top,splits           logits,[tokens],workspace / stats,[ids]   as LOGPROBS
  * LOGPROBS_GRAD rows,vocab                       logits,[tokens],stats,[g_logprob(f32)],[g_entropy(f32)] / dlogits   ld0=of logits,

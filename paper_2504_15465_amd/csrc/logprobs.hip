@@ -760,7 +760,8 @@ int logprobs_plan(const lithos_op_t& op, OpPlan* plan)
         return fail(LITHOS_EINVAL, "logprobs: rows and vocabulary must be positive (got %lld, %lld)", (long long)rows, (long long)vocab);
     if (op.flags & ~(LITHOS_F_IN_F32 | (grad ? LITHOS_F_OUT_F32 : 0u)))
         return fail(LITHOS_EINVAL, grad ? "logprobs_grad: takes IN_F32 and OUT_F32 only" : "logprobs: takes IN_F32 only");
-    if (!(op.fparam[0] > 0.0f) || !(op.fparam[0] < INFINITY)) return fail(LITHOS_EINVAL, "logprobs: the scale (fparam0) must be positive and finite");
+    // exponents are of two: a scale whose product with log2(e) is infinite would make NaN of equal logits
+    if (!(op.fparam[0] > 0.0f) || !(op.fparam[0] * LOG2E < INFINITY)) return fail(LITHOS_EINVAL, "logprobs: the scale (fparam0) must be positive and below 2.3e38");
     if (op.ld[0] < vocab) return fail(LITHOS_EINVAL, "logprobs: row stride of the logits smaller than the vocabulary");
     if (!op.in[0] || reinterpret_cast<uintptr_t>(op.in[0]) % (x32 ? 4 : 2)) return fail(LITHOS_EINVAL, "logprobs: null or misaligned logits");
     if (!aligned_to(op.in[1], 4)) return fail(LITHOS_EINVAL, "logprobs: misaligned tokens");
