@@ -74,6 +74,15 @@ def test_q4_column_blocks_gated(m, a_dt, tiles, blocks, group, k):
     check(c, y, tol)
 
 
+@pytest.mark.parametrize("m", [257, 1000])
+@pytest.mark.parametrize("a_dt", [F32, BF])
+@pytest.mark.parametrize("n,glu", [(301, False), (304, True), (4111, False)])
+def test_q4_rows_of_a_prompt(m, a_dt, n, glu):
+    op, c, y, tol = wide_case(m, n, 712, 64, a_dt, glu)
+    launch(op)
+    check(c, y, tol)
+
+
 @pytest.mark.parametrize("m,tiles,blocks", [c[:1] + c[2:] for c in CASES if c[1] == F32])
 @pytest.mark.parametrize("group", [32, 64, 128])
 def test_q4_every_bit_of_fp32_rows_counts(m, tiles, blocks, group):
