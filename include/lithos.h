@@ -137,7 +137,8 @@ enum {
  *             codes: bytes [ceil(rows/16)][ceil(K/128)][4][16][16]: of 16 weight rows (fourth index) and 128 k, byte 4t + j of
  *             piece p (third index) holds k = 32t + 8p + j in its low and k = 32t + 8p + j + 4 in its high half (t, j = 0..3);
  *             codes beyond the matrix may hold anything.  scales, zeros: bf16 [ceil(rows/16)][ceil(K/group)][16], 16-byte
- *             aligned like the codes; zeros NULL = 8.  More than 16 rows (bf16: 32) are computed 16 (32) at a time, the weights read for each.
+ *             aligned like the codes; zeros NULL = 8.  Computed by groups as s (sum A q - z sum A), so both sums must stay
+ *             finite.  More than 16 rows (bf16: 32) are computed 16 (32) at a time, the weights read for each.
  * KV8_APPEND  batch,tokens,n_kv,d,pos,cap,block  k,v,[positions(i32)],scales / kcodes,vcodes   ld0=row stride of k and v
  *             k, v: rows b*tokens + t (bf16, or fp32 with IN_F32), head h at columns h*d; d = 64 or 128.  Token t of sequence b
  *             becomes position p_b + t of the cache, p_b = positions[b] or pos; a sequence with a negative position takes no
@@ -145,8 +146,9 @@ enum {
  *             E4M3), scales fp32 [2][batch][ceil(cap/block)][n_kv] (keys', values'; written, although an input by place); a code
  *             c stands for scale*c.  block: a multiple of 16 up to 1024.  A block's scale is the largest magnitude / 127 (e4m3:
  *             / 448) of what is appended to it; if the block holds earlier positions and its scale is larger, that stays, and if
- *             smaller, the earlier codes are rounded to the new one (code = round(code * old / new)).  Codes are round(x / scale),
- *             to nearest even, in fp32 quotients.  A block that receives a NaN or an infinity reads as NaN.
+ *             smaller, the earlier codes are rounded to the new one (code = round(code * old / new)), for good: writing the
+ *             position again does not bring back what they lost.  Codes are round(x / scale), to nearest even, in fp32
+ *             quotients.  A block that receives a NaN or an infinity reads as NaN.
  *             Appends to one sequence, and the attention that reads it, follow one another on a queue.
  * ATTN_DEC8   batch,n_q,n_kv,d,keys,cap,splits,block   q,kcodes,vcodes,[workspace],scales,[lens(i32)] / o   ld0=q row stride;
  *             like ATTN_DEC, against KV8_APPEND's cache (E4M3 as there); 1 to 16 query heads per key/value head,    fparam0=scale

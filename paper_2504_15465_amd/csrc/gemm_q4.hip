@@ -17,7 +17,8 @@ static int q4_rows(const lithos_op_t& op)
 // fewer fill the chip.  Time goes with the workgroups of a CU times blocks + x.  A value of C does not depend on the choice.
 // Eight blocks of up to four rows are 12 % slower than four (1 x 2 x 14336 x 4096: 1, 2, 4, 8 blocks 19.5, 19.7, 18.0, 20.3 us
 // a pass); 8 rows 30, 30, 25.5, 22.8, 16 rows 42, 42, 31.7, 26.5; 1 x 4096 x 4096 5.5, 6.2, 8.1, 12.7, 1 x 6144 x 4096 7.2, 6.5,
-// 8.3, 12.8; 24 x 5003 x 2088 bf16 10.6, 8.7, 12.1.
+// 8.3, 12.8; 24 x 5003 x 2088 bf16 10.6, 8.7, 12.1.  The rule misses the best for 1 x 5003 x 2088: two blocks 6.2 us, one 5.6.  With
+// eight blocks of 16 fp32 rows, groups of 32 spill two registers: 16 x 2 x 14336 x 4096 in groups of 32, 64, 128 k 32, 26, 25 us.
 static int q4_blocks(const lithos_op_t& op)
 {
     const bool glu = op.flags & LITHOS_F_GLU, a32 = op.flags & LITHOS_F_IN_F32;

@@ -16,8 +16,11 @@
 // in wavefront order.  sum_k A of a group is one more product, with a column operand of ones, so it comes out in the
 // accumulators' layout.  Scales and zero points come four groups of all tiles at a time, one 16-byte load per lane, and
 // pass through the wavefront's own piece of LDS (a load of their own for each tile and chunk took as long as the codes).
-// Measured: 1 x 4096 x 4096 in 4.9 us, 8 rows against 2 x 14336 x 4096 with gated SiLU in 20.6 us (66 MB, 3.2 TB/s: the rows,
-// 128 KB for each of 224 workgroups, weigh a third of what a CU fetches), 27 x 5003 x 2088 bf16 in 9.0 us.
+// Measured: 1 x 4096 x 4096 in 4.9 us, 8 rows against 2 x 14336 x 4096 with gated SiLU in 20.7 us (66 MB, 3.2 TB/s), 27 x 5003 x
+// 2088 bf16 in 9.0 us.  What a CU fetches bounds the latter two: the rows, 128 KB for each of 224 workgroups and 113 KB for each
+// of 157, and loads behind a wavefront's range, which are issued (clamped to its last chunk) and not used: the caches are asked for
+// 136 MB where 95 are needed, and for 51 where 24 are.  More rows than one operand holds cost the weights again: 32 fp32 rows x 6144 x
+// 4096 13.3 us (bf16 rows 9.1), 512 bf16 rows x 4096 x 4096 44 us.
 #pragma once
 #include "gemm_common.hpp"
 
